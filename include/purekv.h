@@ -39,10 +39,11 @@ typedef enum {
   PUREKV_ERR_WORKSPACE = 3,   /* plan or workspace buffer too small                      */
   PUREKV_ERR_CUDA = 4,        /* a CUDA call failed; text in purekv_last_error           */
   PUREKV_ERR_TIMEOUT = 5,     /* a bounded device-side wait expired (purekv_poll_status) */
-  PUREKV_ERR_BAD_PLAN = 6     /* a kernel found the plan it was handed inconsistent and did not use it (purekv_poll_status) */
+  PUREKV_ERR_BAD_PLAN = 6,    /* a kernel found the plan it was handed inconsistent and did not use it (purekv_poll_status) */
+  PUREKV_ERR_BAD_PAGE = 7     /* a paged call met a page, row or index that does not exist and left it out (purekv_poll_status) */
 } purekv_status;
 
-typedef enum { PUREKV_BF16 = 0, PUREKV_FP32 = 1 } purekv_dtype;
+typedef enum { PUREKV_BF16 = 0, PUREKV_FP32 = 1, PUREKV_E4M3 = 2 /* what a paged cache may hold; no call takes it elsewhere */ } purekv_dtype;
 
 #define PUREKV_FLAG_DENSE_CAUSAL 1u
 #define PUREKV_FLAG_COARSE_BLOCKS 2u
@@ -328,6 +329,83 @@ purekv_status purekv_decode_attention(const void *q, const void *k_cache, const 
                                       int32_t n_kv_heads, int32_t head_dim, purekv_dtype dtype,
                                       float softmax_scale, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- the paged cache: the compressed prompt and the tokens that follow it -------------------------
+ * (The paper's compact cache, Sec. 3.1, is what a prompt leaves; a conversation appends to it.)  K and V of a layer are two
+ * pools of n_pages pages of page_size rows; row s of request r lies in page block_table[r, s / page_size], in its slot
+ * s % page_size.  Layers share the block table and have pools layer_stride apart.  The calls of one step agree on seq_lens: it
+ * counts each request's rows once the step's rows are stored, so that a store writes a request's last rows and the attention
+ * reads all of them.
+ * Strides are in elements and the same for K and V; a row's head_dim elements are contiguous.  [n_pages][page_size][H_kv][d] and
+ * [n_pages][H_kv][page_size][d] are both such layouts.  Strides and pool pointers are multiples of 16 bytes; those of a
+ * dimension of size 1 are not looked at, and no two rows overlap.
+ * With PUREKV_E4M3 a pool holds e4m3 numbers that stand for themselves times k_scale[g], v_scale[g] (device, fp32, one per KV head,
+ * layer after layer; NULL: 1): x is stored as x / scale rounded to the nearest (ties to even), beyond +-448 as +-448.
+ * seq_lens and block_table are read on the device, at the time of the kernel: a captured call follows their contents.  Where
+ * they name a page outside the pool, or a row beyond max_pages * page_size, a store leaves the row out and the attention leaves the
+ * key out, and the status word is set to PUREKV_ERR_BAD_PAGE; nothing outside the pools is touched.  The paged calls compute whatever the word
+ * held before.  Entries of the table behind a request's last page are not looked at. */
+typedef struct {
+  void *k, *v;                                                    /* pools of the (first) layer          */
+  int64_t layer_stride, page_stride, token_stride, head_stride;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  purekv_dtype dtype;                                             /* what the pools hold                 */
+  const float *k_scale, *v_scale;                                 /* device, PUREKV_E4M3 only, nullable  */
+  int32_t n_req, max_pages;                                       /* rows and columns of block_table     */
+  int64_t table_stride;                                           /* elements between its rows           */
+  const int32_t *block_table, *seq_lens;                          /* device                              */
+} purekv_pages;
+
+/* Rotary position embedding.  Pair i of a row turns by positions[axis(i), t] * inv_freq[i] radians, i < rotary_dim / 2: elements
+ * i and i + rotary_dim / 2, or 2i and 2i + 1 with `interleaved`; the row's other elements stay as they are.  The first sections[0]
+ * pairs follow axis 0, the next sections[1] axis 1 and so on, rotary_dim / 2 in all (one axis: text; three: time, height and
+ * width of video tokens).  Positions are the caller's, as a compressed cache has fewer rows than the prompt had tokens.  Angles are
+ * formed in 64 bits, so that far positions keep their fraction of a turn; sine and cosine are fp32. */
+typedef struct {
+  const int32_t *positions;  /* device [n_axes][n_tokens], axis_stride elements between axes */
+  int64_t axis_stride;
+  const double *inv_freq;    /* device [rotary_dim / 2] */
+  int32_t rotary_dim;        /* a multiple of 16, at most head_dim */
+  int32_t n_axes;            /* 1 to 4 */
+  int32_t sections[4];
+  int32_t interleaved;
+} purekv_rope;
+
+/* New tokens of one layer.  q [n_tokens, H, d], k and v [n_tokens, H_kv, d] have strides between tokens and heads (parts of one
+ * projection's output, say).  Request r's tokens are cu_new[r] .. cu_new[r+1]-1 (device [n_req+1], nullable: token r is request
+ * r's one token, n_tokens == n_req); tokens past cu_new[n_req] are only rotated.  The last of them becomes row seq_lens[r]-1; a
+ * request with seq_lens[r] <= 0 stores nothing (padding of a batch).  k rotated and v go into the pages, k rotated into
+ * k_out and q rotated into q_out ([n_tokens, H_kv, d] and [n_tokens, H, d], contiguous; may be k and q themselves where those are
+ * contiguous, and overlap nothing otherwise).  Nullable: q with q_out, k_out, v with pages (a rotation alone: the way into a prefill whose
+ * survivors are compacted later), k with pages and k_out, rope (nothing is rotated).  dtype is that of q, k and v: BF16, for pools of
+ * BF16 or E4M3, or FP32 for FP32 pools.  head_dim a multiple of 16, at most 512; pointers and strides of whole 16 bytes. */
+purekv_status purekv_append_paged(const void *q, int64_t q_token_stride, int64_t q_head_stride, const void *k,
+                                  int64_t k_token_stride, int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                                  int64_t v_head_stride, void *q_out, void *k_out, const purekv_pages *pages,
+                                  const purekv_rope *rope, const int32_t *cu_new, int32_t n_tokens, int32_t n_q_heads,
+                                  int32_t n_kv_heads, int32_t head_dim, purekv_dtype dtype, int32_t *status, void *stream);
+
+/* The rows that a selection kept, all layers at once, into the pages: purekv_compact_kv with the paged cache as its
+ * destination.  Row t of request r, cu_kept[r] <= t < cu_kept[r+1] (device [n_req+1], k_tot = cu_kept[n_req]), is k's and v's token
+ * cu_seqlens[r] + idx[layer, g, t] (idx [n_layers, H_kv, k_tot]; cu_seqlens device [n_req+1]) and becomes row seq_lens[r] - (cu_kept[r+1]
+ * - t), so that the cache's earlier rows, of a shared prefix, say, stay.  An index outside the request sets
+ * PUREKV_ERR_BAD_PAGE and its row is left out; seq_lens[r] <= 0 stores nothing of the request.  k and v [n_layers][total_tokens, H_kv, d] with
+ * layer_stride elements between layers; dtype and head_dim as above. */
+purekv_status purekv_compact_paged(const void *k, const void *v, int64_t layer_stride, int32_t n_layers, const int32_t *idx,
+                                   const int32_t *cu_seqlens, int64_t total_tokens, const int32_t *cu_kept, int32_t k_tot,
+                                   purekv_dtype dtype, const purekv_pages *pages, int32_t *status, void *stream);
+
+/* purekv_decode_attention over the pages of one layer: one new query per request and head, every row of the request visible.
+ * q [n_req, H, d] with strides, o [n_req, H, d] contiguous (may be q itself where that is contiguous), lse (nullable) [n_req, H].
+ * A request with seq_lens[r] <= 0 gets o = 0 and lse = -inf.  head_dim 64 or 128; any number of query heads per KV head; dtype (q and o) BF16 with pools
+ * of BF16 or E4M3, or FP32 with FP32 pools.  max_len only sizes the launch: the longest request that is to be expected,
+ * 0 if unknown; longer requests are served all the same.  ws: purekv_decode_paged_ws_bytes for the same sizes (nullable
+ * when that is 0), not initialised; calls that may run at the same time need one each.  softmax_scale <= 0 means 1/sqrt(d). */
+size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    purekv_dtype dtype);
+purekv_status purekv_decode_paged(const void *q, int64_t q_token_stride, int64_t q_head_stride, void *o, float *lse,
+                                  const purekv_pages *pages, int32_t max_len, int32_t n_q_heads, purekv_dtype dtype,
+                                  float softmax_scale, void *ws, size_t ws_bytes, int32_t *status, void *stream);
+
 /* Failure detection (no counterpart in the paper).  Every wait inside the tensor-core kernels -- on a copy, on a
  * product, on another role of the CTA -- is bounded: when the limit passes the CTA raises the status word to
  * PUREKV_ERR_TIMEOUT, lets its copies and products in flight finish, frees its tensor memory and returns, so the
@@ -341,10 +419,10 @@ purekv_status purekv_decode_attention(const void *q, const void *k_cache, const 
 void purekv_set_wait_limit_ns(uint64_t ns);
 
 /* Synchronises `stream`, copies the device status word to *h_status_out and returns the code it holds
- * (PUREKV_ERR_TIMEOUT or PUREKV_ERR_BAD_PLAN) if it is non-zero, PUREKV_ERR_CUDA if the stream reported an error.
+ * (PUREKV_ERR_TIMEOUT, PUREKV_ERR_BAD_PLAN or PUREKV_ERR_BAD_PAGE) if it is non-zero, PUREKV_ERR_CUDA if the stream reported an error.
  * status == NULL polls the word inside the library that calls made with a NULL status use (one per
  * device, shared by all such calls) and clears it if it was raised.  A raised word makes every later
- * call that uses it return without computing -- the caller's own word stays raised until the caller
+ * tensor-core prefill or score call that uses it return without computing -- the caller's own word stays raised until the caller
  * clears it, the library's until it is polled this way -- so poll after the calls whose results matter. */
 purekv_status purekv_poll_status(const int32_t *status, int32_t *h_status_out, void *stream);
 

@@ -788,6 +788,8 @@ purekv_status purekv_poll_status(const int32_t* status, int32_t* h_out, void* st
   if (h_out) *h_out = v;
   PK_REQUIRE(v != (int32_t)PUREKV_ERR_BAD_PLAN, PUREKV_ERR_BAD_PLAN,
              "device status word is %d: a kernel refused the plan it was handed", v);
+  PK_REQUIRE(v != PUREKV_ERR_BAD_PAGE, PUREKV_ERR_BAD_PAGE,
+             "device status word is %d: a paged call left out a page, row or index that does not exist", v);
   PK_REQUIRE(v == 0, PUREKV_ERR_TIMEOUT, "device status word is %d: a bounded device-side wait expired", v);
   return PUREKV_OK;
 }
