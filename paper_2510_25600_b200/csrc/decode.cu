@@ -14,6 +14,7 @@
 
 #include "cluster.cuh"
 #include "common.cuh"
+#include "decode.cuh"
 
 namespace purekv {
 
@@ -30,12 +31,6 @@ struct Row16<float> {
     f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
   }
 };
-__device__ __forceinline__ float dec_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Folds v[0..N) of the 16 lanes of a half-warp: each step a lane hands half of its values to the partner across
 // `mask` and adds the partner's other half, so the values halve while the lanes summed double.  Afterwards v[0] of
 // lane ch is the full 16-lane sum for head ch >> (4 - log2 N).
@@ -208,18 +203,6 @@ __global__ void __launch_bounds__(kDecThreads) decode_partial_kernel(
 }
 
 // ---- bf16, d = 128 on tensor cores ---------------------------------------------------------------------------
-__device__ __forceinline__ void dec_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t dec_pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
 // A row's reference maximum moves when a logit exceeds it by this (log2).  At 0 it is the largest logit so far, and the heaviest
 // weights are powers of two, exact in bf16: error against 64 bits 1.87e-3 of the norm of the result for 8 requests of 5000 rows, 1.90
 // for 64 of 700, 1.79 for one of 3000 with 16 heads per KV head; at 8, 2.29, 2.31 and 1.97e-3.  (The chunk kernel of before, at 8 but
@@ -246,20 +229,6 @@ constexpr int kClMax = 16;                      // CTAs per cluster
 template <int RW, int ST>
 __host__ __device__ constexpr int cl_warp_bytes() {
   return ST * kClStageBytes > 8 * RW * (128 + 8) * 4 ? ST * kClStageBytes : 8 * RW * (128 + 8) * 4;
-}
-
-__device__ __forceinline__ void dec_ldsm(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void dec_ldsm_t(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ uint32_t dec_mapa(const void* local, uint32_t rank) {
-  uint32_t a;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
-  return a;
 }
 
 // RW: row groups of eight heads in use (1: G <= 8, 2: G <= 16); W warps; ST stages of each warp's ring.

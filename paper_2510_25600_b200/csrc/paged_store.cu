@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
       uint8_t* dst = (is_v ? a.v_pool : a.k_pool) + s_dst[tok] + h * a.view.head_stride;
       if constexpr (E8) {
         const float* sc = is_v ? a.v_scale : a.k_scale;
-        const float scale = sc ? __ldg(sc + h) : 1.f;
+        const float scale = sc ? sc[h] : 1.f;
         reinterpret_cast<uint2*>(dst)[ca] = to_e4m3(x, scale);
         reinterpret_cast<uint2*>(dst)[cb] = to_e4m3(y, scale);
       } else {
@@ -252,13 +252,13 @@ __global__ void __launch_bounds__(256) compact_paged_kernel(const CompactArgs a)
       const int64_t s = __shfl_sync(0xffffffffu, src, row), d = __shfl_sync(0xffffffffu, dst, row);
       const int32_t sc = __shfl_sync(0xffffffffu, scale_at, row);
       if (d < 0) continue;
-      const uint4 ku = __ldg(reinterpret_cast<const uint4*>(a.k + s) + chunk), vu = __ldg(reinterpret_cast<const uint4*>(a.v + s) + chunk);
+      const uint4 ku = reinterpret_cast<const uint4*>(a.k + s)[chunk], vu = reinterpret_cast<const uint4*>(a.v + s)[chunk];
       if constexpr (E8) {
         float f[8];
         Chunk<T>::get(ku, f);
-        reinterpret_cast<uint2*>(a.k_pool + d)[chunk] = to_e4m3(f, a.k_scale ? __ldg(a.k_scale + sc) : 1.f);
+        reinterpret_cast<uint2*>(a.k_pool + d)[chunk] = to_e4m3(f, a.k_scale ? a.k_scale[sc] : 1.f);
         Chunk<T>::get(vu, f);
-        reinterpret_cast<uint2*>(a.v_pool + d)[chunk] = to_e4m3(f, a.v_scale ? __ldg(a.v_scale + sc) : 1.f);
+        reinterpret_cast<uint2*>(a.v_pool + d)[chunk] = to_e4m3(f, a.v_scale ? a.v_scale[sc] : 1.f);
       } else {
         reinterpret_cast<uint4*>(a.k_pool + d)[chunk] = ku;
         reinterpret_cast<uint4*>(a.v_pool + d)[chunk] = vu;
