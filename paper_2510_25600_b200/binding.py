@@ -2,14 +2,17 @@
 
 Every function here has the name of the C entry point it calls and passes torch
 tensors' device pointers straight through, the hot ones by way of the native module
-`_marshal`, the others with ctypes; no step of the method runs in Python or in
+`_marshal` or, the paged calls, `_paged`, the others with ctypes; no step of the method runs in Python or in
 torch.  torch supplies device memory and the current CUDA stream.  Importing
 this module raises if the compiled library is missing: there is no fallback path.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
+import sysconfig
 from typing import Optional, Sequence
 
 import numpy as np
@@ -24,6 +27,21 @@ try:
     from . import _marshal  # noqa: E402  (after the library it calls; built with it, one per Python ABI)
 except ImportError as e:
     raise ImportError(f"{_HERE} holds no _marshal module for this Python: build it with `python -m paper_2510_25600_b200.build`") from e
+
+
+def _load_paged():
+    path = os.path.join(_HERE, f"_paged.torch-{torch.__version__}" + sysconfig.get_config_var("EXT_SUFFIX"))
+    name = __package__ + "._paged"
+    spec = importlib.util.spec_from_file_location(name, path, loader=importlib.machinery.ExtensionFileLoader(name, path))
+    try:
+        module = importlib.util.module_from_spec(spec)
+    except ImportError as e:
+        raise ImportError(f"{_HERE} holds no _paged module for this Python and torch: build it with `python -m paper_2510_25600_b200.build`") from e
+    spec.loader.exec_module(module)
+    return module
+
+
+_paged = _load_paged()
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_BAD_PLAN, ERR_BAD_PAGE = range(8)
 BF16, FP32, E4M3 = 0, 1, 2
@@ -492,74 +510,6 @@ def purekv_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     return out
 
 
-def _paged_code(t: torch.Tensor) -> int:
-    return E4M3 if t.dtype is torch.float8_e4m3fn else _dtype_code(t)
-
-
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
-    device = first.get_device()
-    if device < 0:
-        raise ValueError("the paged calls take tensors on a GPU")
-    for t in others:
-        if t is not None and t.get_device() != device:
-            raise ValueError("the tensors of a paged call lie on one device")
-    return device
-
-
-def _ints(t: torch.Tensor, name: str, shape) -> None:
-    if t.dtype is not torch.int32 or t.shape != shape or (t.dim() and t.stride(-1) != 1 and t.size(-1) > 1):
-        raise ValueError(f"{name}: int32 {list(shape)} with contiguous rows, got {t.dtype} {list(t.shape)} with strides {t.stride()}")
-
-
-def _floats(t: Optional[torch.Tensor], name: str, shape, dtype=torch.float32) -> None:
-    if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
-        raise ValueError(f"{name}: {dtype} {list(shape)}, contiguous, got {t.dtype} {list(t.shape)} with strides {t.stride()}")
-
-
-def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
-           k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], n_layers: int = 0):
-    """The native calls' description of a paged cache; `n_layers` > 0: the pools of so many layers."""
-    shape, strides = k_pages.shape, k_pages.stride()
-    if v_pages.shape != shape or v_pages.stride() != strides or v_pages.dtype is not k_pages.dtype:
-        raise ValueError("k_pages and v_pages have one shape, one layout and one dtype")
-    if len(shape) != (5 if n_layers else 4) or (n_layers and shape[0] != n_layers) or (strides[-1] != 1 and shape[-1] > 1):
-        raise ValueError(f"pools are {'[n_layers, ' if n_layers else '['}n_pages, page_size, H_kv, d] with contiguous rows, got {list(shape)}")
-    layer = 0
-    if n_layers:
-        layer, shape, strides = strides[0], shape[1:], strides[1:]
-    n_req = seq_lens.size(0)
-    _ints(seq_lens, "seq_lens", (n_req,))
-    max_pages = block_table.size(-1)
-    _ints(block_table, "block_table", (n_req, max_pages))
-    scales = (n_layers, shape[2]) if n_layers else (shape[2],)
-    _floats(k_scale, "k_scale", scales)
-    _floats(v_scale, "v_scale", scales)
-    return (1, k_pages.data_ptr(), v_pages.data_ptr(), layer, strides[0], strides[1], strides[2], shape[0], shape[1], shape[2], shape[3],
-            _paged_code(k_pages), None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
-            n_req, max_pages, block_table.stride(0), block_table.data_ptr(), seq_lens.data_ptr())
-
-
-_NO_PAGES = (0, None, None, 0, 0, 0, 0, 0, 1, 0, 0, 0, None, None, 0, 0, 0, None, None)
-_NO_ROPE = (None, 0, None, 0, 0, 0, 0, 0, 0, 0)
-
-
-def _rows(t: torch.Tensor, name: str, n_tokens: int, head_dim: int, dtype: torch.dtype):
-    if t.dim() != 3 or t.size(0) != n_tokens or t.size(2) != head_dim or t.dtype is not dtype or t.stride(2) != 1:
-        raise ValueError(f"{name}: {dtype} [{n_tokens}, heads, {head_dim}] with contiguous rows, got {t.dtype} {list(t.shape)}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
-
-
-def _launch(device: int, native, where: str, *args) -> None:
-    """The native call on the current stream of the tensors' device."""
-    if device == torch.cuda.current_device():
-        status = native(*args, _stream())
-    else:
-        with torch.cuda.device(device):
-            status = native(*args, _stream())
-    if status != OK:
-        raise PureKVError(status, where)
-
-
 def purekv_append_paged(k: Optional[torch.Tensor], v: Optional[torch.Tensor], k_pages: Optional[torch.Tensor], v_pages: Optional[torch.Tensor],
                         block_table: Optional[torch.Tensor], seq_lens: Optional[torch.Tensor], cu_new: Optional[torch.Tensor] = None, *,
                         q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
@@ -570,42 +520,14 @@ def purekv_append_paged(k: Optional[torch.Tensor], v: Optional[torch.Tensor], k_
     fine); k_pages, v_pages [n_pages,page_size,H_kv,d] (or a permuted view of another order of the same); block_table
     [n_req,max_pages], seq_lens [n_req] = rows once these are stored, cu_new [n_req+1] = each request's tokens (None: one
     each), all int32; positions [T] or, with `sections`, [axes,T] int32 and inv_freq [rotary_dim/2] float64 (None: no rotation).
-    Returns q_out, allocated here if q is given without it; k_out [T,H_kv,d] also receives the rotated k.  Without pools, only
-    rotates."""
-    lead = k if k is not None else q
-    if lead is None:
-        raise ValueError("neither k nor q")
-    t, d, dtype = lead.size(0), lead.size(2), lead.dtype
-    device = _same_device(lead, q, v, k_pages, v_pages, block_table, seq_lens, cu_new, q_out, k_out, positions, inv_freq, k_scale, v_scale, status)
-    h, hkv = 0, 0
-    q_args = k_args = v_args = (None, 0, 0)
-    if q is not None:
-        q_args, h = _rows(q, "q", t, d, dtype), q.size(1)
-        if q_out is None:
-            q_out = torch.empty((t, h, d), dtype=dtype, device=q.device)
-        _floats(q_out, "q_out", q.shape, dtype)
-    if k is not None:
-        k_args, hkv = _rows(k, "k", t, d, dtype), k.size(1)
-        _floats(k_out, "k_out", k.shape, dtype)
-    pages = _NO_PAGES
-    if k_pages is not None:
-        if v is None or v.shape != k.shape:
-            raise ValueError("v goes with k into the pages")
-        v_args = _rows(v, "v", t, d, dtype)
-        pages = _pages(k_pages, v_pages, block_table, seq_lens, k_scale, v_scale)
-        if cu_new is not None:
-            _ints(cu_new, "cu_new", (seq_lens.size(0) + 1,))
-    rope = _NO_ROPE
-    if positions is not None:
-        n = inv_freq.size(0)
-        _floats(inv_freq, "inv_freq", (n,), torch.float64)
-        axes = (n,) if sections is None else tuple(sections)
-        _ints(positions, "positions", (t,) if positions.dim() == 1 and len(axes) == 1 else (len(axes), t))
-        if not 1 <= len(axes) <= 4:
-            raise ValueError("1 to 4 sections")
-        rope = (positions.data_ptr(), positions.stride(0), inv_freq.data_ptr(), 2 * n, len(axes), *axes, *(0,) * (4 - len(axes)), interleaved)
-    _launch(device, _marshal.purekv_append_paged, "purekv_append_paged", *q_args, *k_args, *v_args, _ptr(q_out) if q is not None else None,
-            _ptr(k_out), *pages, *rope, _ptr(cu_new), t, h, hkv, d, _dtype_code(lead), _ptr(status))
+    Returns q_out, allocated here if q is given without it; k_out [T,H_kv,d] also receives the rotated k.  Without pools it only
+    rotates.  Shapes, types and devices that do not fit raise ValueError."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    st = _paged.purekv_append_paged(k, v, k_pages, v_pages, block_table, seq_lens, cu_new, q, q_out, k_out, positions, inv_freq, sections,
+                                    interleaved, k_scale, v_scale, status)
+    if st != OK:
+        raise PureKVError(st, "purekv_append_paged")
     return q_out
 
 
@@ -614,21 +536,10 @@ def purekv_compact_paged(k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, ba
                          v_scale: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     """The kept rows of all layers into the pages.  k, v [L,T,H_kv,d]; idx [L,H_kv,K_tot]; k_pages, v_pages
     [L,n_pages,page_size,H_kv,d]; seq_lens [n_req] = rows once these are stored; scales [L,H_kv]."""
-    if k.dim() != 4 or v.shape != k.shape or not _layers_contiguous(k) or not _layers_contiguous(v) or k.stride(0) != v.stride(0) or v.dtype is not k.dtype:
-        raise ValueError("k and v are [n_layers, T, H_kv, d] of one dtype, each layer contiguous")
-    n_layers, t, hkv, d = k.shape
-    device = _same_device(k, v, idx, batch.cu_seqlens, budget.cu_kept, k_pages, v_pages, block_table, seq_lens, k_scale, v_scale, status)
-    pages = _pages(k_pages, v_pages, block_table, seq_lens, k_scale, v_scale, max(1, n_layers))
-    if k_pages.shape[3:] != (hkv, d):
-        raise ValueError("the pages have other heads than k and v")
-    k_tot, n_req = idx.size(-1), seq_lens.size(0)
-    _ints(idx, "idx", (n_layers, hkv, k_tot))
-    if not idx.is_contiguous():
-        raise ValueError("idx: not contiguous")
-    _ints(batch.cu_seqlens, "cu_seqlens", (n_req + 1,))
-    _ints(budget.cu_kept, "cu_kept", (n_req + 1,))
-    _launch(device, _marshal.purekv_compact_paged, "purekv_compact_paged", k.data_ptr(), v.data_ptr(), k.stride(0), n_layers, idx.data_ptr(),
-            batch.cu_seqlens.data_ptr(), t, budget.cu_kept.data_ptr(), k_tot, _dtype_code(k), *pages, _ptr(status))
+    st = _paged.purekv_compact_paged(k, v, idx, batch.cu_seqlens, budget.cu_kept, k_pages, v_pages, block_table, seq_lens, k_scale, v_scale,
+                                     status)
+    if st != OK:
+        raise PureKVError(st, "purekv_compact_paged")
 
 
 def purekv_decode_paged_ws_bytes(n_req: int, max_len: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int = BF16) -> int:
@@ -641,25 +552,17 @@ def purekv_decode_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.T
                         status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One decode step over one layer of the paged cache.  q [n_req,H,d] (a strided view is fine); k_pages, v_pages
     [n_pages,page_size,H_kv,d]; block_table [n_req,max_pages] and seq_lens [n_req] int32; returns o [n_req,H,d].  `max_len`
-    (0: unknown) is the longest request to expect: it sizes the launch, the result does not depend on it."""
-    b, h, d = q.shape
-    device = _same_device(q, k_pages, v_pages, block_table, seq_lens, out, lse, k_scale, v_scale, ws, status)
-    q_args = _rows(q, "q", b, d, q.dtype)
-    pages = _pages(k_pages, v_pages, block_table, seq_lens, k_scale, v_scale)
-    if seq_lens.size(0) != b or k_pages.size(3) != d:
-        raise ValueError(f"q is [{seq_lens.size(0)}, H, {k_pages.size(3)}], got {list(q.shape)}")
+    (0: unknown) is the longest request to expect: it sizes the launch, the result does not depend on it.  `ws`: workspace of
+    purekv_decode_paged_ws_bytes bytes (allocated here when not given)."""
     if out is None:
-        out = torch.empty((b, h, d), dtype=q.dtype, device=q.device)
-    else:
-        _floats(out, "out", q.shape, q.dtype)
-    _floats(lse, "lse", (b, h))
-    code = _dtype_code(q)
-    if ws is None:
-        need = purekv_decode_paged_ws_bytes(b, max_len, h, k_pages.size(2), d, code)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if ws is None and q.dim() == 3 and k_pages.dim() == 4:
+        need = purekv_decode_paged_ws_bytes(q.size(0), max_len, q.size(1), k_pages.size(2), q.size(2), BF16 if q.dtype is torch.bfloat16 else FP32)
         if need:
             ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _launch(device, _marshal.purekv_decode_paged, "purekv_decode_paged", *q_args, out.data_ptr(), _ptr(lse), *pages, max_len, h, code,
-            softmax_scale, _ptr(ws), 0 if ws is None else ws.nbytes, _ptr(status))
+    st = _paged.purekv_decode_paged(q, k_pages, v_pages, block_table, seq_lens, max_len, out, lse, softmax_scale, k_scale, v_scale, ws, status)
+    if st != OK:
+        raise PureKVError(st, "purekv_decode_paged")
     return out
 
 

@@ -1,10 +1,12 @@
 """Builds libpurekv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _marshal, the Python module that passes
-arguments to it (its file name carries the interpreter's ABI, so another Python builds its own).
+arguments to it (its file name carries the interpreter's ABI, so another Python builds its own), and _paged, the same for the paged
+calls, which reads tensors through torch's C++ interface (its file name carries torch's version too).
 
     python -m paper_2510_25600_b200.build [--force] [--verbose]
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -15,6 +17,17 @@ CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libpurekv.so")
 MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+_TORCH = os.path.dirname(importlib.util.find_spec("torch").origin)
+
+
+def _torch_version() -> str:
+    scope: dict = {}
+    with open(os.path.join(_TORCH, "version.py")) as f:
+        exec(f.read(), scope)
+    return str(scope["__version__"])
+
+
+PAGED = os.path.join(_HERE, f"_paged.torch-{_torch_version()}" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["plan.cu", "compact.cu", "decode.cu", "decode_paged.cu", "paged_store.cu", "select.cu", "score.cu", "score_tc.cu", "prefill.cu", "prefill_simt.cu", "prefill_tc.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]
@@ -68,6 +81,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
         # found beside the module at run time: one copy of the library, whether it is loaded through this or by path
         subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", INCLUDE,
                                src, "-o", MARSHAL, "-L", _HERE, "-l:libpurekv.so", "-Wl,-rpath,$ORIGIN"])
+    src = os.path.join(CSRC, "paged_py.cpp")
+    if force or _stale(PAGED, [src, LIB, os.path.join(INCLUDE, "purekv.h")]):
+        cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+        includes = [sysconfig.get_paths()["include"], INCLUDE, os.path.join(_TORCH, "include"),
+                    os.path.join(_TORCH, "include", "torch", "csrc", "api", "include"), cuda]
+        subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", *[f"-I{d}" for d in includes], src, "-o", PAGED,
+                               "-L", _HERE, "-l:libpurekv.so", "-L", os.path.join(_TORCH, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                               "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
     return LIB
 
 

@@ -255,106 +255,12 @@ PyObject* plan_build_host(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return call([&] { return purekv_plan_build_layers_host(b, p, (purekv_dtype)dt, d, h, hkv, n_ctas, layers, out, bytes, info); });
 }
 
-// The descriptor of a paged cache: 18 values; `has` (an integer before them) is 0 where there is none and they are not looked at.
-const purekv_pages* pages_of(Args& a, purekv_pages* p) {
-  const bool has = a.integer() != 0;
-  p->k = a.ptr();
-  p->v = a.ptr();
-  p->layer_stride = a.integer();
-  p->page_stride = a.integer();
-  p->token_stride = a.integer();
-  p->head_stride = a.integer();
-  p->n_pages = a.i32();
-  p->page_size = a.i32();
-  p->n_kv_heads = a.i32();
-  p->head_dim = a.i32();
-  p->dtype = (purekv_dtype)a.i32();
-  p->k_scale = (const float*)a.ptr();
-  p->v_scale = (const float*)a.ptr();
-  p->n_req = a.i32();
-  p->max_pages = a.i32();
-  p->table_stride = a.integer();
-  p->block_table = (const int32_t*)a.ptr();
-  p->seq_lens = (const int32_t*)a.ptr();
-  return has ? p : nullptr;
-}
-
-PyObject* append_paged(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  Args a("append_paged", v, n, 48);
-  const void* q = a.ptr();
-  const int64_t qt = a.integer(), qh = a.integer();
-  const void* k = a.ptr();
-  const int64_t kt = a.integer(), kh = a.integer();
-  const void* vv = a.ptr();
-  const int64_t vt = a.integer(), vh = a.integer();
-  void *qo = a.ptr(), *ko = a.ptr();
-  purekv_pages pg;
-  const purekv_pages* pages = pages_of(a, &pg);
-  purekv_rope rp;
-  rp.positions = (const int32_t*)a.ptr();  // None: no rotation
-  rp.axis_stride = a.integer();
-  rp.inv_freq = (const double*)a.ptr();
-  rp.rotary_dim = a.i32();
-  rp.n_axes = a.i32();
-  for (int i = 0; i < 4; ++i) rp.sections[i] = a.i32();
-  rp.interleaved = a.i32();
-  const int32_t* cu = (const int32_t*)a.ptr();
-  const int32_t tokens = a.i32(), h = a.i32(), hkv = a.i32(), d = a.i32(), dt = a.i32();
-  int32_t* status = (int32_t*)a.ptr();
-  void* stream = a.ptr();
-  if (!a.ok) return nullptr;
-  return call([&] {
-    return purekv_append_paged(q, qt, qh, k, kt, kh, vv, vt, vh, qo, ko, pages, rp.positions ? &rp : nullptr, cu, tokens, h, hkv, d,
-                               (purekv_dtype)dt, status, stream);
-  });
-}
-
-PyObject* compact_paged(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  Args a("compact_paged", v, n, 31);
-  const void *k = a.ptr(), *vv = a.ptr();
-  const int64_t stride = a.integer();
-  const int32_t layers = a.i32();
-  const int32_t *idx = (const int32_t*)a.ptr(), *cu = (const int32_t*)a.ptr();
-  const int64_t tokens = a.integer();
-  const int32_t* ck = (const int32_t*)a.ptr();
-  const int32_t k_tot = a.i32(), dt = a.i32();
-  purekv_pages pg;
-  const purekv_pages* pages = pages_of(a, &pg);
-  int32_t* status = (int32_t*)a.ptr();
-  void* stream = a.ptr();
-  if (!a.ok) return nullptr;
-  return call([&] {
-    return purekv_compact_paged(k, vv, stride, layers, idx, cu, tokens, ck, k_tot, (purekv_dtype)dt, pages, status, stream);
-  });
-}
-
-PyObject* decode_paged(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  Args a("decode_paged", v, n, 32);
-  const void* q = a.ptr();
-  const int64_t qt = a.integer(), qh = a.integer();
-  void* o = a.ptr();
-  float* lse = (float*)a.ptr();
-  purekv_pages pg;
-  const purekv_pages* pages = pages_of(a, &pg);
-  const int32_t max_len = a.i32(), h = a.i32(), dt = a.i32();
-  const float scale = a.f32();
-  void* ws = a.ptr();
-  const size_t ws_bytes = (size_t)a.integer();
-  int32_t* status = (int32_t*)a.ptr();
-  void* stream = a.ptr();
-  if (!a.ok) return nullptr;
-  return call([&] {
-    return purekv_decode_paged(q, qt, qh, o, lse, pages, max_len, h, (purekv_dtype)dt, scale, ws, ws_bytes, status, stream);
-  });
-}
-
 #define PK_METHOD(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PK_METHOD("purekv_st_sparse_prefill", prefill), PK_METHOD("purekv_st_sparse_prefill_layers", prefill_layers),
                          PK_METHOD("purekv_lowlayer_score", score),
                          PK_METHOD("purekv_lowlayer_score_lse", score_lse), PK_METHOD("purekv_lowlayer_score_ex", score_ex),
                          PK_METHOD("purekv_select_topk", select_topk), PK_METHOD("purekv_compact_kv", compact_kv),
-                         PK_METHOD("purekv_decode_attention", decode), PK_METHOD("purekv_append_paged", append_paged),
-                         PK_METHOD("purekv_compact_paged", compact_paged), PK_METHOD("purekv_decode_paged", decode_paged),
+                         PK_METHOD("purekv_decode_attention", decode),
                          PK_METHOD("purekv_plan_build_layers_host", plan_build_host), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
