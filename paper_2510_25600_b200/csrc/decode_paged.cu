@@ -7,8 +7,9 @@
 // Two kernels share everything but the way work reaches a CTA:
 //  * even (CLUSTER): grid (C, heads, requests); a cluster of C CTAs owns one (request, KV head) and its parts meet in distributed
 //    shared memory.  One launch, no workspace.
-//  * balanced: one wave of persistent CTAs; the (request, KV head, tile of keys) triples in that order are cut into equal runs, whatever
-//    the lengths are -- they are read on the device -- and a run goes on loading across the ends of requests.  A request that a cut
+//  * balanced: one wave of persistent CTAs; the (KV head, request, tile of keys) triples in that order are cut into equal runs, whatever
+//    the lengths are -- they are read on the device -- and a run goes on loading across the ends of requests.  (Head by head, so that
+//    CTAs at work on the heads of a request are at the same rows at the same time: those lie side by side in memory.)  A request that a cut
 //    goes through leaves partial results in the workspace, which a second, small kernel joins.
 //
 // Inside a CTA every warp takes TK keys of a tile at a time through a ring of its own in shared memory (cp.async, ST stages), looks the
@@ -51,103 +52,154 @@ constexpr int kDpClusterMax = 16;
 // the CTA shares; and the state of one warp.  load() starts the loads of a group's queries, ready() puts them to use behind a barrier,
 // trip() takes TK keys, finish() leaves the warp's output rows in shared memory and returns (reference, sum) per row.
 
-// bf16 pools: mma.sync, the group's heads are the rows of m16n8k16 tiles.  (M = 16 is far below a tcgen05 tile's 128 rows, and the
-// step is bound by HBM.)  Rows padded by 16 bytes, so that ldmatrix reads eight of them without bank conflicts.
-template <int D_, int RW>
+// On tensor cores a group's heads are the N = 8 columns of m16n8k16 tiles and 16 keys, or 16 of V's columns, their rows: S^T = K Q^T
+// and O^T += V^T P^T, so that up to eight heads waste no row of a tile (half the instructions and the accumulators of tiles with heads as
+// rows).  mma.sync, not tcgen05: a step is bound by HBM, and a warp that goes from S to P to O in registers needs no other's help.
+// A lane holds, for two heads, the logits of two keys; the maxima over the keys are taken across lanes, P is turned into the B operand by
+// a transposition of 8 x 8 blocks, and O's rescaling needs no exchange, since its columns are S's.
+__device__ __forceinline__ uint32_t dp_transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// NT column tiles (of eight heads) and MT row tiles (of 16 keys): references, sums and weights.  sc[..][0, 1]: key g8, heads 2t and 2t + 1
+// of the lane's g8 = lane / 4, t = lane % 4; [2, 3]: key g8 + 8.  Before: logits in log2 units, -inf for keys that are not there; after:
+// the weights.  Returns whether O has to be multiplied by alpha.
+template <int MT, int NT>
+__device__ __forceinline__ bool dp_softmax(float (&sc)[MT][NT][4], float (&m)[NT][2], float (&l)[NT][2], float (&alpha)[NT][2]) {
+  bool grew = false;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      float mx = fmaxf(sc[0][nt][x], sc[0][nt][2 + x]);
+#pragma unroll
+      for (int mt = 1; mt < MT; ++mt) mx = fmaxf(mx, fmaxf(sc[mt][nt][x], sc[mt][nt][2 + x]));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+      const bool up = mx > m[nt][x];
+      alpha[nt][x] = up ? dec_ex2(m[nt][x] - mx) : 1.f;
+      m[nt][x] = up ? mx : m[nt][x];
+      grew |= up;
+    }
+  grew = __any_sync(0xffffffffu, grew);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float ref = m[nt][x] == -INFINITY ? 0.f : m[nt][x];
+      float sum = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        sc[mt][nt][x] = dec_ex2(sc[mt][nt][x] - ref);
+        sc[mt][nt][2 + x] = dec_ex2(sc[mt][nt][2 + x] - ref);
+        sum += sc[mt][nt][x] + sc[mt][nt][2 + x];
+      }
+      l[nt][x] = fmaf(l[nt][x], alpha[nt][x], sum);
+    }
+  return grew;
+}
+template <int N, int NT>
+__device__ __forceinline__ void dp_rescale(float (&o)[N][NT][4], const float (&alpha)[NT][2]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[i][nt][x] *= alpha[nt][x & 1];
+}
+// Sums over the lanes that share heads, and (reference, sum) of each head.
+template <int NT>
+__device__ __forceinline__ void dp_finish_sums(const float (&m)[NT][2], float (&l)[NT][2], float (*ml)[2]) {
+  const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], 4);
+      l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], 8);
+      l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], 16);
+      if (g8 == 0) {
+        ml[8 * nt + 2 * t + x][0] = m[nt][x];
+        ml[8 * nt + 2 * t + x][1] = l[nt][x];
+      }
+    }
+}
+
+// bf16 pools.  Rows padded by 16 bytes, so that ldmatrix reads eight of them without bank conflicts.
+template <int D_, int NT>
 struct Bf16Rows {
-  static constexpr int D = D_, TK = 16, RowBytes = D * 2, KS = RowBytes + 16, VS = RowBytes + 16, R = 8 * RW;
+  static constexpr int D = D_, TK = 16, RowBytes = D * 2, KS = RowBytes + 16, VS = RowBytes + 16, R = 8 * NT;
   using Out = __nv_bfloat16;
   struct Shared {};
-  uint32_t qa[D / 16][4];
-  float o[D / 8][4], m[2], l[2], unit;
+  uint32_t qb[D / 16][NT][2];
+  float o[D / 16][NT][4], m[NT][2], l[NT][2], unit;
 
-  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh, int32_t) {
+  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
     unit = a.scale_log2;
 #pragma unroll
-    for (int rw = 0; rw < RW; ++rw) {
-      const int32_t h = g8 + 8 * rw;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int32_t h = g8 + 8 * nt;
       const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q + r * a.q_tok + (h0 + (h < nh ? h : 0)) * a.q_head) + t;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        qa[ks][rw] = h < nh ? p[ks * 8] : 0u;
-        qa[ks][2 + rw] = h < nh ? p[ks * 8 + 4] : 0u;
+        qb[ks][nt][0] = h < nh ? p[ks * 8] : 0u;
+        qb[ks][nt][1] = h < nh ? p[ks * 8 + 4] : 0u;
       }
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[n][nt][x] = 0.f;
     }
-    if constexpr (RW == 1)
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) qa[ks][1] = qa[ks][3] = 0u;
-#pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
   }
   __device__ __forceinline__ void ready(Shared&) {}
 
   __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared&, int) {
-    const int lane = threadIdx.x & 31, t = lane & 3;
-    const uint32_t k_at = st + ((lane & 7) + 8 * (lane >> 4)) * KS + ((lane >> 3) & 1) * 16;
-    float sc[2][4] = {};
+    const int lane = threadIdx.x & 31, g8 = lane >> 2;
+    const uint32_t k_at = st + ((lane & 7) + 8 * ((lane >> 3) & 1)) * KS + (lane >> 4) * 16;
+    float sc[1][NT][4] = {}, odd[NT][4] = {};  // two chains of products
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      uint32_t b[4];
-      dec_ldsm(k_at + ks * 32, b);
-      dec_mma(sc[0], qa[ks], b[0], b[1]);
-      dec_mma(sc[1], qa[ks], b[2], b[3]);
+      uint32_t k[4];
+      dec_ldsm(k_at + ks * 32, k);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) dec_mma(ks & 1 ? odd[nt] : sc[0][nt], k, qb[ks][nt][0], qb[ks][nt][1]);
     }
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sc[tl][x] = mask >> (8 * tl + 2 * t + (x & 1)) & 1 ? sc[tl][x] * unit : -INFINITY;
-    uint32_t pa[4] = {0u, 0u, 0u, 0u};
+      for (int x = 0; x < 4; ++x) sc[0][nt][x] = mask >> (g8 + 8 * (x >> 1)) & 1 ? (sc[0][nt][x] + odd[nt][x]) * unit : -INFINITY;
+    float alpha[NT][2];
+    if (dp_softmax<1, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
+    uint32_t p[NT][2];
 #pragma unroll
-    for (int rw = 0; rw < RW; ++rw) {
-      float mx = fmaxf(fmaxf(sc[0][2 * rw], sc[0][2 * rw + 1]), fmaxf(sc[1][2 * rw], sc[1][2 * rw + 1]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      if (mx > m[rw]) {  // the same for the four threads of the row
-        const float alpha = dec_ex2(m[rw] - mx);
-        l[rw] *= alpha;
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-          o[n][2 * rw] *= alpha;
-          o[n][2 * rw + 1] *= alpha;
-        }
-        m[rw] = mx;
-      }
-      const float ref = m[rw] == -INFINITY ? 0.f : m[rw];
-      const float p00 = dec_ex2(sc[0][2 * rw] - ref), p01 = dec_ex2(sc[0][2 * rw + 1] - ref);
-      const float p10 = dec_ex2(sc[1][2 * rw] - ref), p11 = dec_ex2(sc[1][2 * rw + 1] - ref);
-      l[rw] += (p00 + p01) + (p10 + p11);
-      pa[rw] = dec_pack_bf16(p00, p01);  // the accumulators of S are the A operand of P V
-      pa[2 + rw] = dec_pack_bf16(p10, p11);
+    for (int nt = 0; nt < NT; ++nt) {
+      p[nt][0] = dp_transpose(dec_pack_bf16(sc[0][nt][0], sc[0][nt][1]));
+      p[nt][1] = dp_transpose(dec_pack_bf16(sc[0][nt][2], sc[0][nt][3]));
     }
-    const uint32_t v_at = st + TK * KS + ((lane & 7) + 8 * ((lane >> 3) & 1)) * VS + (lane >> 4) * 16;
+    const uint32_t v_at = st + TK * KS + ((lane & 7) + 8 * (lane >> 4)) * VS + ((lane >> 3) & 1) * 16;
 #pragma unroll
-    for (int n = 0; n < D / 8; n += 2) {
-      uint32_t b[4];
-      dec_ldsm_t(v_at + n * 16, b);
-      dec_mma(o[n], pa, b[0], b[1]);
-      dec_mma(o[n + 1], pa, b[2], b[3]);
+    for (int n = 0; n < D / 16; ++n) {
+      uint32_t v[4];
+      dec_ldsm_t(v_at + n * 32, v);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) dec_mma(o[n][nt], v, p[nt][0], p[nt][1]);
     }
   }
 
   __device__ __forceinline__ void finish(float* rows, int ld, float (*ml)[2]) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
+    dp_finish_sums<NT>(m, l, ml);
 #pragma unroll
-    for (int rw = 0; rw < RW; ++rw) {
-      l[rw] += __shfl_xor_sync(0xffffffffu, l[rw], 1);
-      l[rw] += __shfl_xor_sync(0xffffffffu, l[rw], 2);
-      if (t == 0) {
-        ml[g8 + 8 * rw][0] = m[rw];
-        ml[g8 + 8 * rw][1] = l[rw];
-      }
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int n = 0; n < D / 8; ++n)
-        *reinterpret_cast<float2*>(rows + (g8 + 8 * rw) * ld + n * 8 + 2 * t) = make_float2(o[n][2 * rw], o[n][2 * rw + 1]);
-    }
+      for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) rows[(8 * nt + 2 * t + (x & 1)) * ld + 16 * n + g8 + 8 * (x >> 1)] = o[n][nt][x];
   }
 };
 
@@ -156,25 +208,25 @@ struct Bf16Rows {
 // logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
 // terms is free, so the queries' fragments are laid out to match.  Of the values, ldmatrix transposes pairs of bytes: a register
 // holds two columns of two keys, which go to two tiles, of the even columns and of the odd ones.
-template <int D_, int RW>
+template <int D_, int NT>
 struct E4m3Rows {
   // Row strides without bank conflicts: for keys eight lanes read 16 bytes of two rows, for values of eight rows.
-  static constexpr int D = D_, TK = 32, RowBytes = D, KS = D == 128 ? 144 : 64, VS = D + 16, R = 8 * RW, CL = D / 64;
+  static constexpr int D = D_, TK = 32, RowBytes = D, KS = D == 128 ? 144 : 64, VS = D + 16, R = 8 * NT, CL = D / 64;
   using Out = __nv_bfloat16;
   struct Shared {};
-  uint32_t qa[D / 16][4];
-  float o[D / 8][4], m[2], l[2], unit[2];
+  uint32_t qb[D / 16][NT][2];
+  float o[D / 16][NT][4], m[NT][2], l[NT][2], unit[NT][2];
 
   static __device__ __forceinline__ uint32_t half2_of(uint16_t pair) {
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(pair));
     return r;
   }
-  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   }
   static __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     uint32_t r;
@@ -182,14 +234,14 @@ struct E4m3Rows {
     return r;
   }
 
-  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh, int32_t) {
+  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
     const float per_key = a.scale_log2 * (a.k_scale ? a.k_scale[g] : 1.f);
 #pragma unroll
-    for (int rw = 0; rw < 2; ++rw) {
-      const int32_t h = g8 + 8 * rw;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int32_t h = g8 + 8 * nt;
       uint32_t w[8 * CL];  // q[16 CL t .. + 16 CL) of head h
-      if (rw < RW && h < nh) {
+      if (h < nh) {
         const uint4* p = reinterpret_cast<const uint4*>(a.q + r * a.q_tok + (h0 + h) * a.q_head) + 2 * CL * t;
 #pragma unroll
         for (int i = 0; i < 2 * CL; ++i) {
@@ -207,98 +259,95 @@ struct E4m3Rows {
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       // elements below 2^15, exact down to 2^-28 of the largest; a head below 2^-112 has logits of nothing and stays as it is
       const bool as_is = top < 15u;
-      const float down = as_is ? 1.f : __uint_as_float((268u - top) << 23), up = as_is ? 1.f : __uint_as_float((top - 14u) << 23);
-      unit[rw] = per_key * up;
+      const float down = as_is ? 1.f : __uint_as_float((268u - top) << 23);
+      const float up = per_key * (as_is ? 1.f : __uint_as_float((top - 14u) << 23));
+      unit[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);  // of the heads whose logits the lane holds
+      unit[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
-      for (int i = 0; i < 8 * CL; ++i) {  // word i: elements 2i, 2i + 1 = k slots of step i / 2, the lower or the upper pair
-        const uint32_t x = pack_half(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
-        qa[i / 2][(i & 1) * 2 + rw] = x;
-      }
+      for (int i = 0; i < 8 * CL; ++i)  // word i: elements 2i, 2i + 1 = k slots of step i / 2, the lower or the upper pair
+        qb[i / 2][nt][i & 1] = pack_half(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[n][nt][x] = 0.f;
     }
-#pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
   }
   __device__ __forceinline__ void ready(Shared&) {}
 
   __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared&, int) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
-    float sc[4][4] = {};
+    float sc[2][NT][4] = {};
 #pragma unroll
-    for (int tl = 0; tl < 4; ++tl)
+    for (int j = 0; j < CL; ++j)
 #pragma unroll
-      for (int j = 0; j < CL; ++j) {
-        uint32_t w[4];
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(st + (8 * tl + g8) * KS + (CL * t + j) * 16) : "memory");
+      for (int mt = 0; mt < 2; ++mt) {
+        uint32_t w[2][4];  // keys g8 and g8 + 8
 #pragma unroll
-        for (int s = 0; s < 4; ++s) mma(sc[tl], qa[4 * j + s], half2_of((uint16_t)w[s]), half2_of((uint16_t)(w[s] >> 16)));
-      }
+        for (int x = 0; x < 2; ++x)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(w[x][0]), "=r"(w[x][1]), "=r"(w[x][2]), "=r"(w[x][3])
+                       : "r"(st + (16 * mt + 8 * x + g8) * KS + (CL * t + j) * 16) : "memory");
 #pragma unroll
-    for (int tl = 0; tl < 4; ++tl)
+        for (int s = 0; s < 4; ++s) {
+          const uint32_t a0 = half2_of((uint16_t)w[0][s]), a2 = half2_of((uint16_t)(w[0][s] >> 16));
+          const uint32_t a1 = half2_of((uint16_t)w[1][s]), a3 = half2_of((uint16_t)(w[1][s] >> 16));
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sc[tl][x] = mask >> (8 * tl + 2 * t + (x & 1)) & 1 ? sc[tl][x] * unit[x >> 1] : -INFINITY;
-    uint32_t pa[2][4] = {};
-#pragma unroll
-    for (int rw = 0; rw < RW; ++rw) {
-      float mx = fmaxf(sc[0][2 * rw], sc[0][2 * rw + 1]);
-#pragma unroll
-      for (int tl = 1; tl < 4; ++tl) mx = fmaxf(mx, fmaxf(sc[tl][2 * rw], sc[tl][2 * rw + 1]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      if (mx > m[rw]) {
-        const float alpha = dec_ex2(m[rw] - mx);
-        l[rw] *= alpha;
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-          o[n][2 * rw] *= alpha;
-          o[n][2 * rw + 1] *= alpha;
+          for (int nt = 0; nt < NT; ++nt) mma(sc[mt][nt], a0, a1, a2, a3, qb[4 * j + s][nt][0], qb[4 * j + s][nt][1]);
         }
-        m[rw] = mx;
       }
-      const float ref = m[rw] == -INFINITY ? 0.f : m[rw];
 #pragma unroll
-      for (int tl = 0; tl < 4; ++tl) {
-        const float p0 = dec_ex2(sc[tl][2 * rw] - ref), p1 = dec_ex2(sc[tl][2 * rw + 1] - ref);
-        l[rw] += p0 + p1;
-        pa[tl >> 1][(tl & 1) * 2 + rw] = pack_half(p0, p1);
-      }
-    }
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
+    float alpha[NT][2];
+    if (dp_softmax<2, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
     const uint32_t v_at = st + TK * KS + ((lane & 7) + 8 * ((lane >> 3) & 1)) * VS + (lane >> 4) * 16;
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int mt = 0; mt < 2; ++mt) {
+      uint32_t p[NT][2];
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {  // 32 columns
-        uint32_t b[4];
-        dec_ldsm_t(v_at + half * 16 * VS + c * 32, b);
+      for (int nt = 0; nt < NT; ++nt) {
+        p[nt][0] = dp_transpose(pack_half(sc[mt][nt][0], sc[mt][nt][1]));
+        p[nt][1] = dp_transpose(pack_half(sc[mt][nt][2], sc[mt][nt][3]));
+      }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {  // 16 columns: b[2i] of keys 2t, 2t + 1 and b[2i + 1] of keys 2t + 8, 2t + 9
-          const uint32_t a0 = half2_of((uint16_t)b[2 * i]), a1 = half2_of((uint16_t)(b[2 * i] >> 16));
-          const uint32_t c0 = half2_of((uint16_t)b[2 * i + 1]), c1 = half2_of((uint16_t)(b[2 * i + 1] >> 16));
-          mma(o[4 * c + 2 * i], pa[half], __byte_perm(a0, a1, 0x5410), __byte_perm(c0, c1, 0x5410));
-          mma(o[4 * c + 2 * i + 1], pa[half], __byte_perm(a0, a1, 0x7632), __byte_perm(c0, c1, 0x7632));
+      for (int c = 0; c < D / 32; ++c) {  // 32 columns: b[0] and b[1] keys 2t, 2t + 1 and 2t + 8, 2t + 9 of the first 16, b[2] and b[3] of the others
+        uint32_t b[4], lo[4], hi[4];
+        dec_ldsm_t(v_at + mt * 16 * VS + c * 32, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo[i] = half2_of((uint16_t)b[i]);
+          hi[i] = half2_of((uint16_t)(b[i] >> 16));
+        }
+        uint32_t even[4], odd[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          even[i] = __byte_perm(lo[i], hi[i], 0x5410);
+          odd[i] = __byte_perm(lo[i], hi[i], 0x7632);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma(o[2 * c][nt], even[0], even[2], even[1], even[3], p[nt][0], p[nt][1]);
+          mma(o[2 * c + 1][nt], odd[0], odd[2], odd[1], odd[3], p[nt][0], p[nt][1]);
         }
       }
+    }
   }
 
   __device__ __forceinline__ void finish(float* rows, int ld, float (*ml)[2]) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
+    dp_finish_sums<NT>(m, l, ml);
 #pragma unroll
-    for (int rw = 0; rw < RW; ++rw) {
-      l[rw] += __shfl_xor_sync(0xffffffffu, l[rw], 1);
-      l[rw] += __shfl_xor_sync(0xffffffffu, l[rw], 2);
-      if (t == 0) {
-        ml[g8 + 8 * rw][0] = m[rw];
-        ml[g8 + 8 * rw][1] = l[rw];
-      }
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c)
-        *reinterpret_cast<float4*>(rows + (g8 + 8 * rw) * ld + 16 * c + 4 * t) =
-            make_float4(o[2 * c][2 * rw], o[2 * c + 1][2 * rw], o[2 * c][2 * rw + 1], o[2 * c + 1][2 * rw + 1]);
-    }
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<float2*>(rows + (8 * nt + 2 * t + (x & 1)) * ld + 32 * c + 16 * (x >> 1) + 2 * g8) = make_float2(o[2 * c][nt][x], o[2 * c + 1][nt][x]);
   }
 };
 
@@ -316,7 +365,7 @@ struct Fp32Rows {
   float staged[kQPerThread];
   float o[GP][E], m[GP], l[GP];
 
-  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh, int32_t) {
+  __device__ __forceinline__ void load(const DecodePagedArgs& a, Shared&, int32_t r, int32_t g, int32_t h0, int32_t nh) {
 #pragma unroll
     for (int i = 0; i < kQPerThread; ++i) {
       const int32_t x = threadIdx.x + i * (int32_t)blockDim.x, h = x / D;
@@ -445,7 +494,7 @@ __device__ __forceinline__ void dp_store4(__nv_bfloat16* dst, float4 v) {
 template <>
 __device__ __forceinline__ void dp_store4(float* dst, float4 v) { *reinterpret_cast<float4*>(dst) = v; }
 
-template <class E, int W, int ST, bool CLUSTER, int OCC>
+template <class E, int W, int ST, bool CLUSTER, bool WHOLE, int OCC>
 __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_constant__ DecodePagedArgs a) {
   constexpr int D = E::D, R = E::R, TK = E::TK, TILE = W * TK, kThreads = W * 32, kStage = dp_stage_bytes<E>(), LD = dp_ld<E>();
   constexpr int kWarpBytes = dp_warp_bytes<E, ST>();
@@ -457,8 +506,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   __shared__ __align__(16) float s_part[CLUSTER ? R * D : 1];          // what the cluster's CTAs send this one: [source][head][its columns]
   __shared__ __align__(8) float s_pml[CLUSTER ? kDpClusterMax : 1][R][2];  // every CTA's (reference, sum) per head
   __shared__ int64_t s_scan[W + 1];
-  __shared__ int64_t s_at;
-  __shared__ int32_t s_req;
+  __shared__ int32_t s_req, s_tile;
 
   const int32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int32_t C = CLUSTER ? (int32_t)gridDim.x : 1, rank = CLUSTER ? (int32_t)blockIdx.x : 0;
@@ -472,10 +520,17 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const int32_t len = a.view.seq_lens[r];
     return min(max(len, 0), capacity);
   };
-  // the next request that has rows (there is one, or the lengths have changed under the kernel: then the last request, as it is)
-  auto next_request = [&](int32_t& i, int32_t& rows) {
-    rows = 0;
-    while (rows == 0 && i + 1 < a.n_req) rows = rows_of(++i);
+  // the next request that has rows, or the next head's first one (there is one, or the lengths have changed under the kernel: then
+  // whatever request comes last)
+  auto next_request = [&](int32_t& i, int32_t& v, int32_t& rows) {
+    do {
+      if (i + 1 == a.n_req) {
+        if (v + 1 == a.v_heads) break;
+        i = -1;
+        ++v;
+      }
+      rows = rows_of(++i);
+    } while (rows == 0);
   };
   auto tiles_of = [&](int32_t n) { return (n + TILE - 1) / TILE; };
 
@@ -499,16 +554,19 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     for (int x = 16; x >= 1; x /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
     if (lane == 0) s_scan[warp] = sum;
     __syncthreads();
-    for (int w = 0; w < W; ++w) all += s_scan[w];
-    all *= a.v_heads;
+    int64_t per_head = 0;
+    for (int w = 0; w < W; ++w) per_head += s_scan[w];
+    all = per_head * a.v_heads;
     runs = min((int64_t)ctas, all);  // (each of a tile or more)
     first = c < runs ? all * c / runs : all;
     total = c < runs ? all * (c + 1) / runs - first : 0;
-    // the request in which tile `first` lies: running sums over the requests, kThreads at a time
+    vh = total > 0 ? (int32_t)(first / per_head) : 0;
+    const int64_t of_head = first - vh * per_head;
+    // the request in which tile `of_head` lies: running sums over the requests, kThreads at a time
     int64_t before = 0;
     for (int32_t i0 = 0; i0 < a.n_req && total > 0; i0 += kThreads) {
       const int32_t i = i0 + tid;
-      const int64_t mine = i < a.n_req ? (int64_t)tiles_of(rows_of(i)) * a.v_heads : 0;
+      const int64_t mine = i < a.n_req ? (int64_t)tiles_of(rows_of(i)) : 0;
       int64_t upto = mine;
 #pragma unroll
       for (int x = 1; x < 32; x *= 2) {
@@ -524,19 +582,17 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         chunk += s_scan[w];
       }
       upto += before;
-      if (upto - mine <= first && first < upto) {
+      if (upto - mine <= of_head && of_head < upto) {
         s_req = i;
-        s_at = first - (upto - mine);
+        s_tile = (int32_t)(of_head - (upto - mine));
       }
       before += chunk;
-      if (before > first) break;
+      if (before > of_head) break;
     }
     __syncthreads();
     r = total > 0 ? s_req : 0;
     n = total > 0 ? rows_of(r) : 0;
-    const int64_t at = total > 0 ? s_at : 0;
-    vh = n ? (int32_t)(at / tiles_of(n)) : 0;
-    tile = n ? (int32_t)(at - (int64_t)vh * tiles_of(n)) : 0;
+    tile = total > 0 ? s_tile : 0;
     for (int32_t i = c; i < a.n_req; i += ctas) {
       const int32_t len = a.view.seq_lens[i];
       if (len > capacity && tid == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
@@ -553,14 +609,17 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   int32_t fr = r, fvh = vh, ftile = tile, fn = n;
   int64_t f_left = total;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dp_smem) + (uint32_t)warp * kWarpBytes;
-  struct Look {  // the page of lane's row (there < 0: no such row is wanted), its slot and its KV head
-    int32_t page, slot, g;
+  // The page of a row, its slot there and its KV head.  WHOLE (a page holds whole trips): of the trip's first row, `there` of whose
+  // rows are wanted; otherwise of row `lane` of the trip, `there` 1 if it is wanted.
+  struct Look {
+    int32_t page, slot, g, there;
   };
   auto look = [&]() {
-    Look k = {-1, -1, 0};
+    Look k = {-1, 0, 0, 0};
     if (f_left > 0) {
-      const int32_t row = ftile * TILE + warp * TK + lane;
-      if (lane < TK && row < fn) {
+      const int32_t row = ftile * TILE + warp * TK + (WHOLE ? 0 : lane);
+      k.there = WHOLE ? min(max(fn - row, 0), TK) : lane < TK && row < fn;
+      if (k.there > 0) {
         const uint32_t p = a.view.page_size.quotient((uint32_t)row);
         k.slot = row - (int32_t)(p * a.view.page_size.d);
         k.page = a.view.table[(int64_t)fr * a.view.table_stride + p];
@@ -569,34 +628,59 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       --f_left;
       if (++ftile == tiles_of(fn)) {
         ftile = 0;
-        if (++fvh == a.v_heads && !CLUSTER) {
-          fvh = 0;
-          if (f_left > 0) next_request(fr, fn);
-        }
+        if (!CLUSTER && f_left > 0) next_request(fr, fvh, fn);
       }
     }
     return k;
   };
   constexpr int CPR = E::RowBytes / 16, RPI = 32 / CPR;  // 16-byte chunks of a row, rows of a warp's request
+  auto copy = [](uint32_t dst, const uint8_t* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); };
+  auto copy_or_zero = [](uint32_t dst, const uint8_t* src, bool there) {  // zeros for rows that do not exist: nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
+  };
   auto fetch = [&](int32_t stage, const Look& k) {
-    int64_t off = k.slot >= 0 ? a.view.offset(k.page, (uint32_t)k.slot) : -1;
-    const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0);
-    if (__ballot_sync(0xffffffffu, k.slot >= 0) != mask && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
-    if (lane == 0) s_mask[warp][stage] = mask;
-    if (mask) {
-      off += (int64_t)k.g * a.view.head_stride;
-      const uint32_t dst = ring + (uint32_t)stage * kStage + (lane / CPR) * E::KS + (lane % CPR) * 16;
-      const uint32_t dst_v = ring + (uint32_t)stage * kStage + TK * E::KS + (lane / CPR) * E::VS + (lane % CPR) * 16;
+    const uint32_t dst = ring + (uint32_t)stage * kStage + (lane / CPR) * E::KS + (lane % CPR) * 16;
+    const uint32_t dst_v = ring + (uint32_t)stage * kStage + TK * E::KS + (lane / CPR) * E::VS + (lane % CPR) * 16;
+    const int64_t off = k.there > 0 ? a.view.offset(k.page, (uint32_t)k.slot) : -1;
+    uint32_t mask;
+    if constexpr (WHOLE) {
+      mask = off < 0 ? 0u : k.there == 32 ? 0xffffffffu : (1u << k.there) - 1u;
+      if (k.there > 0 && off < 0 && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+      if (mask) {
+        const int64_t from = off + (int64_t)k.g * a.view.head_stride + (lane / CPR) * a.view.token_stride + (lane % CPR) * 16;
+        const uint8_t *kp = a.k_pool + from, *vp = a.v_pool + from;
+        const int64_t step = RPI * a.view.token_stride;
+        if (k.there == TK) {
 #pragma unroll
-      for (int i = 0; i < TK / RPI; ++i) {
-        const int row = i * RPI + lane / CPR;
-        const int64_t src = __shfl_sync(0xffffffffu, off, row) + (lane % CPR) * 16;
-        const uint32_t bytes = mask >> row & 1 ? 16u : 0u;  // zeros for rows that do not exist
-        const int64_t from = bytes ? src : 0;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * RPI * E::KS), "l"(a.k_pool + from), "r"(bytes) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst_v + i * RPI * E::VS), "l"(a.v_pool + from), "r"(bytes) : "memory");
+          for (int i = 0; i < TK / RPI; ++i, kp += step, vp += step) {
+            copy(dst + i * RPI * E::KS, kp);
+            copy(dst_v + i * RPI * E::VS, vp);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < TK / RPI; ++i, kp += step, vp += step) {
+            const bool there = i * RPI + lane / CPR < k.there;
+            copy_or_zero(dst + i * RPI * E::KS, there ? kp : a.k_pool, there);
+            copy_or_zero(dst_v + i * RPI * E::VS, there ? vp : a.v_pool, there);
+          }
+        }
+      }
+    } else {
+      mask = __ballot_sync(0xffffffffu, off >= 0);
+      if (__ballot_sync(0xffffffffu, k.there > 0) != mask && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+      if (mask) {
+        const int64_t mine = off + (int64_t)k.g * a.view.head_stride;
+#pragma unroll
+        for (int i = 0; i < TK / RPI; ++i) {
+          const int row = i * RPI + lane / CPR;
+          const int64_t from = __shfl_sync(0xffffffffu, mine, row) + (lane % CPR) * 16;
+          const bool there = mask >> row & 1;
+          copy_or_zero(dst + i * RPI * E::KS, a.k_pool + (there ? from : 0), there);
+          copy_or_zero(dst_v + i * RPI * E::VS, a.v_pool + (there ? from : 0), there);
+        }
       }
     }
+    if (lane == 0) s_mask[warp][stage] = mask;
     asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
   };
   Look next;
@@ -618,7 +702,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   };
   int32_t g, h0, nh;
   heads_at(vh, g, h0, nh);
-  e.load(a, s_e, r, g, h0, nh, warp);
+  e.load(a, s_e, r, g, h0, nh);
   e.ready(s_e);
   __syncthreads();
 
@@ -656,13 +740,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
     const int32_t r_done = r, h0_done = h0, nh_done = nh, g_done = g, vh_done = vh, n_done = n;
     if (!CLUSTER && !end_of_run) {  // the next request's queries, while this one's results are joined
-      if (++vh == a.v_heads) {
-        vh = 0;
-        next_request(r, n);
-      }
+      next_request(r, vh, n);
       tile = 0;
       heads_at(vh, g, h0, nh);
-      e.load(a, s_e, r, g, h0, nh, warp);
+      e.load(a, s_e, r, g, h0, nh);
     }
     __syncthreads();
     if constexpr (CLUSTER) {
@@ -764,53 +845,83 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   }
 }
 
-// Joins the parts of the requests that cuts went through: grid (CTAs of the balanced form, heads of a tile), a thread per column.
+// Joins the parts of the requests that cuts went through: grid (half of the balanced form's CTAs, heads of a tile), a block looks
+// after two CTAs' chains.  Each D / 4 threads take eight parts at a time, all loads of which are asked for before the first is used, and
+// run a softmax of their own over them; the groups meet in shared memory.
 template <class E>
-__global__ void __launch_bounds__(E::D) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
-  constexpr int D = E::D, R = E::R;
-  __shared__ float s_w[D], s_red[D / 32];
-  const int32_t c = threadIdx.x, h = blockIdx.y, lane = c & 31, warp = c >> 5;
+__global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
+  constexpr int D = E::D, R = E::R, kGroup = D / 4, kGroups = 256 / kGroup, kAtOnce = 8;
+  __shared__ float s_ml[kGroups][2];
+  __shared__ __align__(16) float4 s_acc[kGroups][kGroup];
+  const int32_t h = blockIdx.y, grp = threadIdx.x / kGroup, c = threadIdx.x % kGroup;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const ChainRecord chain = reinterpret_cast<const ChainRecord*>(a.chains)[blockIdx.x];
-  if (chain.parts == 0) return;
-  const int32_t g = chain.vh / a.blocks, b = chain.vh - g * a.blocks;
-  if (h >= min(R, a.group - b * R)) return;
-  auto slot = [&](int32_t i) { return a.part + (i == 0 ? 2 * (int64_t)blockIdx.x + 1 : 2 * ((int64_t)blockIdx.x + i)) * dp_part_floats<E>(); };
-  float top = -INFINITY;
-  for (int32_t i = c; i < chain.parts; i += D) top = fmaxf(top, dp_seen(slot(i)[R * D + h], slot(i)[R * D + R + h]));
+  const ChainRecord both[2] = {reinterpret_cast<const ChainRecord*>(a.chains)[2 * blockIdx.x], reinterpret_cast<const ChainRecord*>(a.chains)[2 * blockIdx.x + 1]};
 #pragma unroll
-  for (int x = 16; x >= 1; x /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-  if (lane == 0) s_red[warp] = top;
-  __syncthreads();
-  top = s_red[0];
+  for (int which = 0; which < 2; ++which) {
+    const ChainRecord chain = both[which];
+    const int32_t g = a.blocks == 1 ? chain.vh : chain.vh / a.blocks, b = chain.vh - g * a.blocks;
+    if (chain.parts == 0 || h >= min(R, a.group - b * R)) continue;  // the same for the block
+    const int64_t cta = 2 * blockIdx.x + which;
+    float ref = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int32_t i0 = grp; i0 < chain.parts; i0 += kAtOnce * kGroups) {
+      float mi[kAtOnce], li[kAtOnce];
+      float4 v[kAtOnce];
 #pragma unroll
-  for (int w = 1; w < D / 32; ++w) top = fmaxf(top, s_red[w]);
-  const float ref = dp_finite(top);
-  float acc = 0.f, l = 0.f;
-  for (int32_t i0 = 0; i0 < chain.parts; i0 += D) {
-    const int32_t np = min(D, chain.parts - i0);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int32_t i = i0 + k * kGroups;
+        mi[k] = -INFINITY;
+        li[k] = 0.f;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < chain.parts) {
+          const float* slot = a.part + (2 * (cta + i) + (i == 0 ? 1 : 0)) * dp_part_floats<E>();
+          mi[k] = slot[R * D + h];
+          li[k] = slot[R * D + R + h];
+          v[k] = *reinterpret_cast<const float4*>(slot + h * D + 4 * c);
+        }
+      }
+      float top = ref;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, dp_seen(mi[k], li[k]));
+      const float alpha = dp_weight(ref, l, dp_finite(top));
+      ref = top;
+      l *= alpha;
+      acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float w = dp_weight(mi[k], li[k], dp_finite(ref));
+        l = fmaf(w, li[k], l);
+        acc.x = fmaf(w, v[k].x, acc.x); acc.y = fmaf(w, v[k].y, acc.y); acc.z = fmaf(w, v[k].z, acc.z); acc.w = fmaf(w, v[k].w, acc.w);
+      }
+    }
+    if (c == 0) {
+      s_ml[grp][0] = ref;
+      s_ml[grp][1] = l;
+    }
+    s_acc[grp][c] = acc;
     __syncthreads();
-    if (c < np) {
-      const float li = slot(i0 + c)[R * D + R + h];
-      s_w[c] = dp_weight(slot(i0 + c)[R * D + h], li, ref);
-      l = fmaf(s_w[c], li, l);
+    if (grp == 0) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) top = fmaxf(top, dp_seen(s_ml[i][0], s_ml[i][1]));
+      const float to = dp_finite(top);
+      acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const float w = dp_weight(s_ml[i][0], s_ml[i][1], to);
+        const float4 v = s_acc[i][c];
+        l = fmaf(w, s_ml[i][1], l);
+        acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+      }
+      const int64_t hq = (int64_t)chain.r * a.n_q_heads + g * a.group + b * R + h;
+      const float inv = (a.v_scale ? a.v_scale[g] : 1.f) / l;
+      dp_store4(reinterpret_cast<typename E::Out*>(a.o) + hq * D + 4 * c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      if (c == 0 && a.lse) a.lse[hq] = (to + log2f(l)) * 0.6931471805599453f;
     }
     __syncthreads();
-#pragma unroll 4
-    for (int32_t i = 0; i < np; ++i) acc = fmaf(s_w[i], slot(i0 + i)[h * D + c], acc);
   }
-#pragma unroll
-  for (int x = 16; x >= 1; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-  __syncthreads();
-  if (lane == 0) s_red[warp] = l;
-  __syncthreads();
-  l = 0.f;
-#pragma unroll
-  for (int w = 0; w < D / 32; ++w) l += s_red[w];
-  const int64_t hq = (int64_t)chain.r * a.n_q_heads + g * a.group + b * R + h;
-  reinterpret_cast<typename E::Out*>(a.o)[hq * D + c] = (typename E::Out)(acc * ((a.v_scale ? a.v_scale[g] : 1.f) / l));
-  if (c == 0 && a.lse) a.lse[hq] = (ref + log2f(l)) * 0.6931471805599453f;
 }
 
 // ---- launching ----------------------------------------------------------------------------------------------------------
@@ -831,9 +942,9 @@ struct DpLaunch {
   }
 };
 
-template <class E, int W, int ST, int OCC>
+template <class E, int W, int ST, bool WHOLE, int OCC>
 static purekv_status launch_even(const DecodePagedArgs& a, int32_t cl, cudaStream_t stream) {
-  auto kernel = decode_paged_kernel<E, W, ST, true, OCC>;
+  auto kernel = decode_paged_kernel<E, W, ST, true, WHOLE, OCC>;
   static std::atomic<uint64_t> smem_allowed{0}, wide_allowed{0};
   const purekv_status st = allow_max_dynamic_smem(kernel, smem_allowed);
   if (st != PUREKV_OK) return st;
@@ -859,20 +970,20 @@ static purekv_status launch_even(const DecodePagedArgs& a, int32_t cl, cudaStrea
   return PUREKV_OK;
 }
 
-template <class E, int W, int ST, int OCC>
+template <class E, int W, int ST, bool WHOLE, int OCC>
 static purekv_status launch_balanced(const DecodePagedArgs& a, int32_t ctas, cudaStream_t stream) {
-  auto kernel = decode_paged_kernel<E, W, ST, false, OCC>;
+  auto kernel = decode_paged_kernel<E, W, ST, false, WHOLE, OCC>;
   static std::atomic<uint64_t> smem_allowed{0};
   const purekv_status st = allow_max_dynamic_smem(kernel, smem_allowed);
   if (st != PUREKV_OK) return st;
   DpLaunch l(dim3((unsigned)ctas), W * 32, (size_t)W * dp_warp_bytes<E, ST>(), stream);
   PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a));
-  DpLaunch j(dim3((unsigned)ctas, (unsigned)std::min(E::R, a.group)), E::D, 0, stream);
+  DpLaunch j(dim3((unsigned)(ctas / 2), (unsigned)std::min(E::R, a.group)), 256, 0, stream);
   PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E>, a));
   return PUREKV_OK;
 }
 
-constexpr int32_t kDpCtas = 148;  // CTAs of the balanced form: one per SM
+constexpr int32_t kDpCtas = 296;  // CTAs of the balanced form: two per SM
 
 // How a call is launched: C CTAs per (request, head) in a cluster, or 0 for the balanced form.
 struct DpForm {
@@ -884,10 +995,14 @@ static DpForm dp_form(int64_t base, int64_t bound) {
   return {bound <= 128 * (int64_t)c * 2 ? c : 0};
 }
 
-template <class E, int ST8>
+template <class E, int ST8, bool WHOLE>
 static purekv_status launch_form(const DecodePagedArgs& a, const DpForm& f, cudaStream_t stream) {
-  if (f.cluster) return launch_even<E, 8, ST8, 1>(a, f.cluster, stream);
-  return launch_balanced<E, 8, ST8, 1>(a, kDpCtas, stream);
+  if (f.cluster) return launch_even<E, 8, ST8, WHOLE, 1>(a, f.cluster, stream);
+  return launch_balanced<E, 4, ST8, WHOLE, 2>(a, kDpCtas, stream);
+}
+template <class E, int ST8>
+static purekv_status launch_rows(const DecodePagedArgs& a, const DpForm& f, cudaStream_t stream) {
+  return a.view.page_size.d % E::TK == 0 ? launch_form<E, ST8, true>(a, f, stream) : launch_form<E, ST8, false>(a, f, stream);
 }
 
 static int32_t dp_rows(int32_t group, purekv_dtype dtype) { return dtype == PUREKV_FP32 ? (group <= 2 ? 2 : 8) : group <= 8 ? 8 : 16; }
@@ -963,15 +1078,15 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   cudaStream_t sm = (cudaStream_t)stream;
   const bool wide = pages->head_dim == 128;
   if (dtype == PUREKV_FP32) {
-    if (rows == 2) return wide ? launch_form<Fp32Rows<128, 2>, 3>(a, form, sm) : launch_form<Fp32Rows<64, 2>, 3>(a, form, sm);
-    return wide ? launch_form<Fp32Rows<128, 8>, 3>(a, form, sm) : launch_form<Fp32Rows<64, 8>, 3>(a, form, sm);
+    if (rows == 2) return wide ? launch_rows<Fp32Rows<128, 2>, 3>(a, form, sm) : launch_rows<Fp32Rows<64, 2>, 3>(a, form, sm);
+    return wide ? launch_rows<Fp32Rows<128, 8>, 3>(a, form, sm) : launch_rows<Fp32Rows<64, 8>, 3>(a, form, sm);
   }
   if (pages->dtype == PUREKV_E4M3) {
-    if (rows == 8) return wide ? launch_form<E4m3Rows<128, 1>, 3>(a, form, sm) : launch_form<E4m3Rows<64, 1>, 5>(a, form, sm);
-    return wide ? launch_form<E4m3Rows<128, 2>, 2>(a, form, sm) : launch_form<E4m3Rows<64, 2>, 5>(a, form, sm);
+    if (rows == 8) return wide ? launch_rows<E4m3Rows<128, 1>, 3>(a, form, sm) : launch_rows<E4m3Rows<64, 1>, 5>(a, form, sm);
+    return wide ? launch_rows<E4m3Rows<128, 2>, 2>(a, form, sm) : launch_rows<E4m3Rows<64, 2>, 5>(a, form, sm);
   }
-  if (rows == 8) return wide ? launch_form<Bf16Rows<128, 1>, 3>(a, form, sm) : launch_form<Bf16Rows<64, 1>, 5>(a, form, sm);
-  return wide ? launch_form<Bf16Rows<128, 2>, 3>(a, form, sm) : launch_form<Bf16Rows<64, 2>, 5>(a, form, sm);
+  if (rows == 8) return wide ? launch_rows<Bf16Rows<128, 1>, 3>(a, form, sm) : launch_rows<Bf16Rows<64, 1>, 5>(a, form, sm);
+  return wide ? launch_rows<Bf16Rows<128, 2>, 3>(a, form, sm) : launch_rows<Bf16Rows<64, 2>, 5>(a, form, sm);
 }
 
 }  // extern "C"
