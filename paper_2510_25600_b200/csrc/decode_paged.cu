@@ -25,6 +25,7 @@
 #include "decode.cuh"
 #include "paged.cuh"
 #include "paged_args.cuh"
+#include "tc_util.cuh"
 
 namespace purekv {
 
@@ -41,11 +42,26 @@ struct DecodePagedArgs {
   void* o;
   float* lse;
   int32_t* status;
-  int32_t* chains;   // balanced form: per CTA what it leaves to be joined (ChainRecord)
-  float* part;       //   and two slots of partial results per CTA
+  // balanced form: per run what it leaves to be joined (ChainRecord) and two slots of partial results; CTAs at work at once; long and
+  // short runs of a head; the limit of waits
+  int32_t* chains;
+  float* part;
+  int32_t at_once, n_long, n_short;
+  uint64_t wait_ns;
 };
 
 constexpr int kDpClusterMax = 16;
+constexpr int kDpGroups = 128;   // of requests: their running sums of tiles lie in shared memory
+constexpr int kDpSteals = 8;     // answers to requests for runs that a CTA keeps: more than runs its loads can be ahead of its products
+// Three quarters of a CTA's share of the tiles make its long run; the rest is cut into short runs, three for every CTA at work, of four
+// tiles at least, which go to whichever CTA asks next.
+constexpr int kDpAtOnce = 296, kDpShorts = 3, kDpShortest = 4;  // CTAs at work: two per SM
+
+// Tiles of one head: `left` of them, from tile `tile` of request r (n rows) on, tile `at` of the head's.
+struct DpRun {
+  int32_t id, vh, r, tile, n;
+  int64_t at, left;
+};
 
 // ---- the three ways of multiplying --------------------------------------------------------------------------------------
 // Each has: TK keys per trip, KS and VS bytes between rows of K and V in shared memory, R query heads per tile, `Shared` for what
@@ -127,10 +143,25 @@ __device__ __forceinline__ void dp_finish_sums(const float (&m)[NT][2], float (&
     }
 }
 
-// bf16 pools.  Rows padded by 16 bytes, so that ldmatrix reads eight of them without bank conflicts.
-template <int D_, int NT>
+// How rows lie in a stage.  Copied by threads (SW false): one after the other, each padded so that no two of the rows that an
+// instruction reads share banks.  Copied by the copy engine (SW true): in parts of 128 bytes, a part's rows one after the other, the
+// 16-byte chunks of a row swizzled (by 128 bytes; 64-byte rows by 64).  In both, `at` is the address of chunk c of row `row`, given
+// that the rows of one instruction agree in row - row % 8.
+template <int TK, int RowBytes, int Stride, bool SW>
+struct RowsAt {
+  static __device__ __forceinline__ uint32_t at(uint32_t base, int row, int c) {
+    if constexpr (!SW) return base + row * Stride + c * 16;
+    else if constexpr (RowBytes == 64) return base + row * 64 + ((c ^ (row >> 1 & 3)) * 16);
+    else return base + (c >> 3) * (TK * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16);
+  }
+};
+
+// bf16 pools.  Padding of 16 bytes, so that ldmatrix reads eight rows without bank conflicts.
+template <int D_, int NT, bool SW_>
 struct Bf16Rows {
-  static constexpr int D = D_, TK = 16, RowBytes = D * 2, KS = RowBytes + 16, VS = RowBytes + 16, R = 8 * NT;
+  static constexpr bool SW = SW_;
+  static constexpr int D = D_, TK = 16, RowBytes = D * 2, KS = RowBytes + (SW ? 0 : 16), VS = KS, R = 8 * NT;
+  using At = RowsAt<TK, RowBytes, KS, SW>;
   using Out = __nv_bfloat16;
   struct Shared {};
   uint32_t qb[D / 16][NT][2];
@@ -160,12 +191,11 @@ struct Bf16Rows {
 
   __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared&, int) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2;
-    const uint32_t k_at = st + ((lane & 7) + 8 * ((lane >> 3) & 1)) * KS + (lane >> 4) * 16;
     float sc[1][NT][4] = {}, odd[NT][4] = {};  // two chains of products
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
       uint32_t k[4];
-      dec_ldsm(k_at + ks * 32, k);
+      dec_ldsm(At::at(st, (lane & 7) + 8 * ((lane >> 3) & 1), 2 * ks + (lane >> 4)), k);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) dec_mma(ks & 1 ? odd[nt] : sc[0][nt], k, qb[ks][nt][0], qb[ks][nt][1]);
     }
@@ -181,11 +211,10 @@ struct Bf16Rows {
       p[nt][0] = dp_transpose(dec_pack_bf16(sc[0][nt][0], sc[0][nt][1]));
       p[nt][1] = dp_transpose(dec_pack_bf16(sc[0][nt][2], sc[0][nt][3]));
     }
-    const uint32_t v_at = st + TK * KS + ((lane & 7) + 8 * (lane >> 4)) * VS + ((lane >> 3) & 1) * 16;
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) {
       uint32_t v[4];
-      dec_ldsm_t(v_at + n * 32, v);
+      dec_ldsm_t(At::at(st + TK * KS, (lane & 7) + 8 * (lane >> 4), 2 * n + ((lane >> 3) & 1)), v);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) dec_mma(o[n][nt], v, p[nt][0], p[nt][1]);
     }
@@ -208,10 +237,13 @@ struct Bf16Rows {
 // logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
 // terms is free, so the queries' fragments are laid out to match.  Of the values, ldmatrix transposes pairs of bytes: a register
 // holds two columns of two keys, which go to two tiles, of the even columns and of the odd ones.
-template <int D_, int NT>
+template <int D_, int NT, bool SW_>
 struct E4m3Rows {
+  static constexpr bool SW = SW_;
   // Row strides without bank conflicts: for keys eight lanes read 16 bytes of two rows, for values of eight rows.
-  static constexpr int D = D_, TK = 32, RowBytes = D, KS = D == 128 ? 144 : 64, VS = D + 16, R = 8 * NT, CL = D / 64;
+  static constexpr int D = D_, TK = 32, RowBytes = D, KS = SW ? D : D == 128 ? 144 : 64, VS = SW ? D : D + 16, R = 8 * NT, CL = D / 64;
+  using KAt = RowsAt<TK, RowBytes, KS, SW>;
+  using VAt = RowsAt<TK, RowBytes, VS, SW>;
   using Out = __nv_bfloat16;
   struct Shared {};
   uint32_t qb[D / 16][NT][2];
@@ -288,7 +320,7 @@ struct E4m3Rows {
         for (int x = 0; x < 2; ++x)
           asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                        : "=r"(w[x][0]), "=r"(w[x][1]), "=r"(w[x][2]), "=r"(w[x][3])
-                       : "r"(st + (16 * mt + 8 * x + g8) * KS + (CL * t + j) * 16) : "memory");
+                       : "r"(KAt::at(st, 16 * mt + 8 * x + g8, CL * t + j)) : "memory");
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const uint32_t a0 = half2_of((uint16_t)w[0][s]), a2 = half2_of((uint16_t)(w[0][s] >> 16));
@@ -305,7 +337,6 @@ struct E4m3Rows {
         for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
     float alpha[NT][2];
     if (dp_softmax<2, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
-    const uint32_t v_at = st + TK * KS + ((lane & 7) + 8 * ((lane >> 3) & 1)) * VS + (lane >> 4) * 16;
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       uint32_t p[NT][2];
@@ -317,7 +348,7 @@ struct E4m3Rows {
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {  // 32 columns: b[0] and b[1] keys 2t, 2t + 1 and 2t + 8, 2t + 9 of the first 16, b[2] and b[3] of the others
         uint32_t b[4], lo[4], hi[4];
-        dec_ldsm_t(v_at + mt * 16 * VS + c * 32, b);
+        dec_ldsm_t(VAt::at(st + TK * KS, 16 * mt + (lane & 7) + 8 * ((lane >> 3) & 1), 2 * c + (lane >> 4)), b);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           lo[i] = half2_of((uint16_t)b[i]);
@@ -353,9 +384,11 @@ struct E4m3Rows {
 
 // fp32 pools: CUDA cores (tf32 would not keep fp32's accuracy).  For the logits a lane takes 32 elements of one key and all heads; for
 // the output D / 32 columns of every key.
-template <int D_, int GP>
+template <int D_, int GP, bool SW_>
 struct Fp32Rows {
-  static constexpr int D = D_, TK = D == 64 ? 16 : 8, RowBytes = D * 4, KS = RowBytes + 16, VS = RowBytes + 16, R = GP, E = D / 32;
+  static constexpr bool SW = SW_;
+  static constexpr int D = D_, TK = D == 64 ? 16 : 8, RowBytes = D * 4, KS = RowBytes + (SW ? 0 : 16), VS = KS, R = GP, E = D / 32;
+  using At = RowsAt<TK, RowBytes, KS, SW>;
   using Out = float;
   struct Shared {
     float q[GP][D];
@@ -396,7 +429,7 @@ struct Fp32Rows {
     for (int c = 0; c < 8; ++c) {
       float4 k;
       asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                   : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(st + key * KS + part * 128 + c * 16) : "memory");
+                   : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(At::at(st, key, part * 8 + c)) : "memory");
 #pragma unroll
       for (int h = 0; h < GP; ++h) {
         const float4 q = *reinterpret_cast<const float4*>(&s.q[h][part * 32 + c * 4]);
@@ -426,14 +459,13 @@ struct Fp32Rows {
       }
     }
     __syncwarp();
-    const uint32_t v_at = st + TK * KS + lane * (4 * E);
 #pragma unroll
     for (int j = 0; j < TK; ++j) {
       float v[E];
       if constexpr (E == 2)
-        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(v_at + j * VS) : "memory");
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(At::at(st + TK * KS, j, lane >> 1) + (lane & 1) * 8) : "memory");
       else
-        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(v_at + j * VS) : "memory");
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(At::at(st + TK * KS, j, lane)) : "memory");
 #pragma unroll
       for (int h = 0; h < GP; ++h) {
         const float p = s.p[warp][j][h];
@@ -462,9 +494,9 @@ struct Fp32Rows {
 // ---- the kernel ---------------------------------------------------------------------------------------------------------
 template <class E>
 __host__ __device__ constexpr int dp_stage_bytes() { return E::TK * (E::KS + E::VS); }
-// A warp's output rows start eight banks apart; they are laid over the stage that the warp used last.
+// A warp's output rows start eight banks apart where there is room; they are laid over the stage that the warp used last.
 template <class E>
-__host__ __device__ constexpr int dp_ld() { return E::D + 8; }
+__host__ __device__ constexpr int dp_ld() { return E::R * (E::D + 8) * 4 <= dp_stage_bytes<E>() ? E::D + 8 : E::D; }
 template <class E, int ST>
 __host__ __device__ constexpr int dp_warp_bytes() {
   static_assert(ST == 1 || E::R * dp_ld<E>() * 4 <= dp_stage_bytes<E>(), "a warp's rows fit a stage");
@@ -474,8 +506,8 @@ __host__ __device__ constexpr int dp_warp_bytes() {
 template <class E>
 __host__ __device__ constexpr int64_t dp_part_floats() { return (int64_t)E::R * (E::D + 2); }
 
-// What a CTA of the balanced form leaves: the request and virtual head whose first part it is (in its second slot), and how many
-// parts there are (the others in the first slots of the CTAs that follow); 0: nothing.
+// What a run of the balanced form leaves: the request and virtual head whose first part it is (in its second slot), and how many
+// parts there are (the others in the first slots of the head's runs that follow); 0: nothing.
 struct ChainRecord {
   int32_t r, vh, parts, pad;
 };
@@ -494,19 +526,36 @@ __device__ __forceinline__ void dp_store4(__nv_bfloat16* dst, float4 v) {
 template <>
 __device__ __forceinline__ void dp_store4(float* dst, float4 v) { *reinterpret_cast<float4*>(dst) = v; }
 
-template <class E, int W, int ST, bool CLUSTER, bool WHOLE, int OCC>
-__global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_constant__ DecodePagedArgs a) {
+// How rows come into shared memory: each by its own page (cp.async); a trip's rows from one page (cp.async), where a page holds whole
+// trips; the same by the copy engine.
+enum DpLoad { kDpRows, kDpWhole, kDpEngine };
+// The pools as the copy engine sees them, in bytes: (128 of a row, slot of a page, part of a row, head, page).
+struct DpMaps {
+  CUtensorMap k, v;
+};
+
+template <class E, int W, int ST, bool CLUSTER, DpLoad LOAD, int OCC>
+__global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_constant__ DecodePagedArgs a, const __grid_constant__ DpMaps maps) {
+  constexpr bool WHOLE = LOAD != kDpRows;
+  static_assert(E::SW == (LOAD == kDpEngine), "the copy engine swizzles");
   constexpr int D = E::D, R = E::R, TK = E::TK, TILE = W * TK, kThreads = W * 32, kStage = dp_stage_bytes<E>(), LD = dp_ld<E>();
   constexpr int kWarpBytes = dp_warp_bytes<E, ST>();
   using Out = typename E::Out;
-  extern __shared__ __align__(16) uint8_t dp_smem[];
+  extern __shared__ __align__(16) uint8_t dp_smem_raw[];
+  // (the swizzle counts from multiples of 1024 bytes)
+  uint8_t* const dp_smem = LOAD == kDpEngine ? dp_smem_raw + (-(int32_t)__cvta_generic_to_shared(dp_smem_raw) & 1023) : dp_smem_raw;
   __shared__ float s_ml[W][R][2];
   __shared__ uint32_t s_mask[W][ST];
+  __shared__ __align__(8) uint64_t s_full[LOAD == kDpEngine ? W : 1][ST];  // a stage's copies have arrived
+  __shared__ int s_late;
   __shared__ __align__(16) typename E::Shared s_e;
   __shared__ __align__(16) float s_part[CLUSTER ? R * D : 1];          // what the cluster's CTAs send this one: [source][head][its columns]
   __shared__ __align__(8) float s_pml[CLUSTER ? kDpClusterMax : 1][R][2];  // every CTA's (reference, sum) per head
-  __shared__ int64_t s_scan[W + 1];
-  __shared__ int32_t s_req, s_tile;
+  __shared__ int64_t s_sum[W];
+  __shared__ int64_t s_tiles[CLUSTER ? 1 : kDpGroups];                // running sums of the requests' tiles, by groups of requests
+  __shared__ __align__(16) ulonglong2 s_stolen[CLUSTER ? 1 : kDpSteals];  // answers to this CTA's requests for runs
+  __shared__ __align__(8) uint64_t s_answered[CLUSTER ? 1 : kDpSteals];
+  __shared__ DpRun s_run[CLUSTER ? 1 : W][kDpSteals];                 // per warp: the runs that its loads have entered
 
   const int32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int32_t C = CLUSTER ? (int32_t)gridDim.x : 1, rank = CLUSTER ? (int32_t)blockIdx.x : 0;
@@ -520,94 +569,148 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const int32_t len = a.view.seq_lens[r];
     return min(max(len, 0), capacity);
   };
-  // the next request that has rows, or the next head's first one (there is one, or the lengths have changed under the kernel: then
-  // whatever request comes last)
-  auto next_request = [&](int32_t& i, int32_t& v, int32_t& rows) {
-    do {
-      if (i + 1 == a.n_req) {
-        if (v + 1 == a.v_heads) break;
-        i = -1;
-        ++v;
-      }
-      rows = rows_of(++i);
-    } while (rows == 0);
+  // the next request that has rows (there is one, or the lengths have changed under the kernel: then the last request)
+  auto next_request = [&](int32_t& i, int32_t& rows) {
+    while (i + 1 < a.n_req && (rows = rows_of(++i)) == 0) {}
   };
   auto tiles_of = [&](int32_t n) { return (n + TILE - 1) / TILE; };
 
-  // This CTA's tiles: `total` of them, from tile `tile` of (request r, virtual head vh) on.
-  int32_t r, vh, tile, n;
-  int64_t total, all = 0, runs = 0, first = 0;
+  // The work at hand: `left` tiles from tile `tile` of (request r with n rows, virtual head vh) on.
+  DpRun run = {};
+  int64_t all = 0, long_tiles = 0, short_tiles = 0;  // of a head: all tiles, those of a long and of a short run
+  // run b: of head b % v_heads the (b / v_heads)th, first the long ones
+  auto starts_at = [&](int32_t j) {
+    return min(all, j <= a.n_long ? j * long_tiles : a.n_long * long_tiles + (j - a.n_long) * short_tiles);
+  };
+  auto take = [&](int32_t b) {
+    const int32_t j = b / a.v_heads;
+    DpRun x = {b, b - j * a.v_heads, 0, 0, 0, starts_at(j), 0};
+    x.left = starts_at(j + 1) - x.at;
+    if (x.left > 0) {
+      // the group of requests in which tile x.at lies, then the request
+      uint32_t hit = __ballot_sync(0xffffffffu, s_tiles[lane * (kDpGroups / 32) + kDpGroups / 32 - 1] > x.at);
+      const int32_t first = (__ffs(hit) - 1) * (kDpGroups / 32);
+      hit = __ballot_sync(0xffffffffu, lane < kDpGroups / 32 && s_tiles[first + lane % (kDpGroups / 32)] > x.at);
+      const int32_t group = first + __ffs(hit) - 1, per_group = (a.n_req + kDpGroups - 1) / kDpGroups;
+      int64_t before = group > 0 ? s_tiles[group - 1] : 0;
+      for (int32_t i0 = group * per_group; i0 < a.n_req; i0 += 32) {
+        const int32_t rows = i0 + lane < a.n_req ? rows_of(i0 + lane) : 0;
+        int64_t upto = tiles_of(rows);
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += y;
+        }
+        hit = __ballot_sync(0xffffffffu, before + upto > x.at);
+        if (hit) {
+          const int32_t l0 = __ffs(hit) - 1;
+          x.r = i0 + l0;
+          x.n = __shfl_sync(0xffffffffu, rows, l0);
+          x.tile = (int32_t)(x.at - (before + __shfl_sync(0xffffffffu, upto, l0) - tiles_of(x.n)));
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
+    return x;
+  };
+  // Thread 0 asks for a run that no CTA has started; the answer comes to its slot and barrier.
+  auto ask = [&](int32_t k) {
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(&s_stolen[k % kDpSteals]), bar = (uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]);
+    tc::mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(slot), "r"(bar) : "memory");
+  };
+  // The run of answer k, or -1.
+  auto answer = [&](int32_t k) {
+    volatile int late = 0;
+    if (!tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]), (uint32_t)(k / kDpSteals) & 1u, &late, a.wait_ns)) {
+      atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
+      return -1;
+    }
+    const volatile ulonglong2& h = s_stolen[k % kDpSteals];
+    const uint64_t lo = h.x, hi = h.y;
+    uint32_t yes, b;
+    asm volatile(
+        "{\n .reg .b128 h;\n .reg .pred p;\n mov.b128 h, {%2, %3};\n clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n"
+        " selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n}\n"
+        : "=r"(yes), "=r"(b) : "l"(lo), "l"(hi));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // read before a later answer overwrites it
+    return yes ? (int32_t)b : -1;
+  };
+  ChainRecord* const chains = reinterpret_cast<ChainRecord*>(a.chains);
+  // Once a run is empty all further ones are: what no CTA has started need not be.
+  auto drain = [&](int32_t k) {
+    for (int32_t b = 0;; ++k) {
+      ask(k);
+      if ((b = answer(k)) < 0) return;
+      chains[b].parts = 0;
+    }
+  };
   if constexpr (CLUSTER) {
-    r = blockIdx.z;
-    vh = blockIdx.y;
-    n = rows_of(r);
-    if (a.view.seq_lens[r] > capacity && tid == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
-    const int32_t share = (tiles_of(n) + C - 1) / C;
-    tile = min(rank * share, tiles_of(n));
-    total = min(share, tiles_of(n) - tile);
+    run = {0, (int32_t)blockIdx.y, (int32_t)blockIdx.z, 0, rows_of(blockIdx.z), 0, 0};
+    if (a.view.seq_lens[run.r] > capacity && tid == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+    const int32_t tiles = tiles_of(run.n), share = (tiles + C - 1) / C;
+    run.tile = min(rank * share, tiles);
+    run.left = min(share, tiles - run.tile);
   } else {
-    const int32_t ctas = gridDim.x, c = blockIdx.x;
-    // all tiles, and requests without rows: their outputs are zero
-    int64_t sum = 0;
-    for (int32_t i = tid; i < a.n_req; i += kThreads) sum += tiles_of(rows_of(i));
+    if (tid < kDpSteals) tc::mbar_init((uint32_t)__cvta_generic_to_shared(&s_answered[tid]), 1);
+    if (LOAD == kDpEngine && lane < ST) tc::mbar_init((uint32_t)__cvta_generic_to_shared(&s_full[warp][lane]), 1);
+    if (tid == 0) s_late = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    constexpr int kPer = kDpGroups / kThreads;  // groups of a thread
+    const int32_t per_group = (a.n_req + kDpGroups - 1) / kDpGroups;
+    int64_t mine[kPer], sum = 0;
 #pragma unroll
-    for (int x = 16; x >= 1; x /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-    if (lane == 0) s_scan[warp] = sum;
-    __syncthreads();
-    int64_t per_head = 0;
-    for (int w = 0; w < W; ++w) per_head += s_scan[w];
-    all = per_head * a.v_heads;
-    runs = min((int64_t)ctas, all);  // (each of a tile or more)
-    first = c < runs ? all * c / runs : all;
-    total = c < runs ? all * (c + 1) / runs - first : 0;
-    vh = total > 0 ? (int32_t)(first / per_head) : 0;
-    const int64_t of_head = first - vh * per_head;
-    // the request in which tile `of_head` lies: running sums over the requests, kThreads at a time
-    int64_t before = 0;
-    for (int32_t i0 = 0; i0 < a.n_req && total > 0; i0 += kThreads) {
-      const int32_t i = i0 + tid;
-      const int64_t mine = i < a.n_req ? (int64_t)tiles_of(rows_of(i)) : 0;
-      int64_t upto = mine;
+    for (int x = 0; x < kPer; ++x) {
+      const int32_t i0 = (tid * kPer + x) * per_group;
+      for (int32_t i = i0; i < min(i0 + per_group, a.n_req); ++i) sum += tiles_of(rows_of(i));
+      mine[x] = sum;
+    }
+    int64_t upto = sum;
 #pragma unroll
-      for (int x = 1; x < 32; x *= 2) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, upto, x);
-        if (lane >= x) upto += y;
-      }
-      __syncthreads();
-      if (lane == 31) s_scan[warp] = upto;
-      __syncthreads();
-      int64_t chunk = 0;
-      for (int w = 0; w < W; ++w) {
-        if (w < warp) upto += s_scan[w];
-        chunk += s_scan[w];
-      }
-      upto += before;
-      if (upto - mine <= of_head && of_head < upto) {
-        s_req = i;
-        s_tile = (int32_t)(of_head - (upto - mine));
-      }
-      before += chunk;
-      if (before > of_head) break;
+    for (int d = 1; d < 32; d *= 2) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
     }
+    if (lane == 31) s_sum[warp] = upto;
     __syncthreads();
-    r = total > 0 ? s_req : 0;
-    n = total > 0 ? rows_of(r) : 0;
-    tile = total > 0 ? s_tile : 0;
-    for (int32_t i = c; i < a.n_req; i += ctas) {
-      const int32_t len = a.view.seq_lens[i];
-      if (len > capacity && tid == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
-      if (rows_of(i) > 0) continue;
-      for (int32_t x = tid; x < a.n_q_heads * (D / 4); x += kThreads)
-        dp_store4(reinterpret_cast<Out*>(a.o) + (int64_t)i * a.n_q_heads * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f));
-      if (a.lse)
-        for (int32_t x = tid; x < a.n_q_heads; x += kThreads) a.lse[(int64_t)i * a.n_q_heads + x] = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w < warp) upto += s_sum[w];
+      all += s_sum[w];
     }
-    if (tid == 0) reinterpret_cast<ChainRecord*>(a.chains)[c].parts = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) s_tiles[tid * kPer + x] = upto - sum + mine[x];
+    __syncthreads();
+    long_tiles = min(all, max((int64_t)1, all * a.v_heads * 3 / 4 / a.at_once));
+    short_tiles = max((int64_t)kDpShortest, (max((int64_t)0, all - a.n_long * long_tiles) + a.n_short - 1) / a.n_short);
+    if (tid == 0) chains[blockIdx.x].parts = 0;
+    run = take(blockIdx.x);
+    if (run.left <= 0) {
+      if (tid == 0) drain(0);
+      return;
+    }
+    if (tid == 0) ask(0);
   }
 
-  // ---- loads.  The cursor (fr, fvh, ftile, fn) runs ahead of the products, over the ends of requests.
-  int32_t fr = r, fvh = vh, ftile = tile, fn = n;
-  int64_t f_left = total;
+  // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier).
+  auto arrived = [&](int32_t stage, uint32_t phase) {
+    if constexpr (LOAD == kDpEngine) {
+      const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]);
+      if (tc::mbar_try_wait(bar, phase) || tc::mbar_wait(bar, phase, &s_late, a.wait_ns)) return true;
+      atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
+      volatile int again = 0;  // the copies may still come: once more as long, before the stage is given up
+      return tc::mbar_wait(bar, phase, &again, a.wait_ns);
+    } else {
+      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+      return true;
+    }
+  };
+
+  // ---- loads.  The cursor runs ahead of the products, over the ends of requests and of runs.
+  DpRun f = run;
+  int32_t f_answers = 0, f_runs = 1;  // answers read, runs entered
+  bool f_more = !CLUSTER, f_empty = false;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dp_smem) + (uint32_t)warp * kWarpBytes;
   // The page of a row, its slot there and its KV head.  WHOLE (a page holds whole trips): of the trip's first row, `there` of whose
   // rows are wanted; otherwise of row `lane` of the trip, `there` 1 if it is wanted.
@@ -616,19 +719,38 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   };
   auto look = [&]() {
     Look k = {-1, 0, 0, 0};
-    if (f_left > 0) {
-      const int32_t row = ftile * TILE + warp * TK + (WHOLE ? 0 : lane);
-      k.there = WHOLE ? min(max(fn - row, 0), TK) : lane < TK && row < fn;
+    if constexpr (!CLUSTER) {
+      if (f.left == 0 && f_more) {
+        const int32_t b = answer(f_answers++);
+        f_more = false;
+        if (b >= 0) {
+          if (tid == 0) chains[b].parts = 0;
+          const DpRun x = take(b);
+          if (x.left > 0) {
+            f = x;
+            f_more = true;
+            if (tid == 0) ask(f_answers);
+            if (lane == 0) s_run[warp][f_runs % kDpSteals] = x;
+            ++f_runs;
+          } else {
+            f_empty = true;
+          }
+        }
+      }
+    }
+    if (f.left > 0) {
+      const int32_t row = f.tile * TILE + warp * TK + (WHOLE ? 0 : lane);
+      k.there = WHOLE ? min(max(f.n - row, 0), TK) : lane < TK && row < f.n;
       if (k.there > 0) {
         const uint32_t p = a.view.page_size.quotient((uint32_t)row);
         k.slot = row - (int32_t)(p * a.view.page_size.d);
-        k.page = a.view.table[(int64_t)fr * a.view.table_stride + p];
+        k.page = a.view.table[(int64_t)f.r * a.view.table_stride + p];
       }
-      k.g = a.blocks == 1 ? fvh : fvh / a.blocks;
-      --f_left;
-      if (++ftile == tiles_of(fn)) {
-        ftile = 0;
-        if (!CLUSTER && f_left > 0) next_request(fr, fvh, fn);
+      k.g = a.blocks == 1 ? f.vh : f.vh / a.blocks;
+      --f.left;
+      if (++f.tile == tiles_of(f.n)) {
+        f.tile = 0;
+        if (!CLUSTER && f.left > 0) next_request(f.r, f.n);
       }
     }
     return k;
@@ -643,7 +765,24 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const uint32_t dst_v = ring + (uint32_t)stage * kStage + TK * E::KS + (lane / CPR) * E::VS + (lane % CPR) * 16;
     const int64_t off = k.there > 0 ? a.view.offset(k.page, (uint32_t)k.slot) : -1;
     uint32_t mask;
-    if constexpr (WHOLE) {
+    if constexpr (LOAD == kDpEngine) {
+      mask = off < 0 ? 0u : k.there == 32 ? 0xffffffffu : (1u << k.there) - 1u;
+      if (lane == 0) {
+        if (k.there > 0 && off < 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+        const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), to = ring + (uint32_t)stage * kStage;
+        if (mask) {  // whole trips: what lies behind the request's last row is masked (keys) or overwritten (values) later
+          tc::mbar_expect_tx(bar, 2 * TK * E::RowBytes);
+          auto load = [&](uint32_t dst, const CUtensorMap* map) {
+            asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                         ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(k.slot), "r"(0), "r"(k.g), "r"(k.page) : "memory");
+          };
+          load(to, &maps.k);
+          load(to + TK * E::KS, &maps.v);
+        } else {
+          tc::mbar_arrive(bar);  // (the barrier's phases stay in step with the stages)
+        }
+      }
+    } else if constexpr (WHOLE) {
       mask = off < 0 ? 0u : k.there == 32 ? 0xffffffffu : (1u << k.there) - 1u;
       if (k.there > 0 && off < 0 && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
       if (mask) {
@@ -681,7 +820,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
     }
     if (lane == 0) s_mask[warp][stage] = mask;
-    asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
+    if constexpr (LOAD != kDpEngine) asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
   };
   Look next;
   {
@@ -701,49 +840,75 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     nh = min(R, a.group - b * R);
   };
   int32_t g, h0, nh;
-  heads_at(vh, g, h0, nh);
-  e.load(a, s_e, r, g, h0, nh);
+  heads_at(run.vh, g, h0, nh);
+  e.load(a, s_e, run.r, g, h0, nh);
   e.ready(s_e);
   __syncthreads();
 
-  int32_t stage = 0;
-  bool from_start = tile == 0;  // whether this CTA has the request's first tile
-  for (int64_t i = 0;; ++i) {
-    bool end_of_request = true, end_of_run = true;
-    if (i < total) {
+  int32_t stage = 0, c_runs = 1;  // c_runs: runs entered by the products
+  uint32_t phase = 0;
+  bool from_start = run.tile == 0;  // whether this run has the request's first tile
+  while (true) {
+    bool end_of_request = true;
+    if (run.left > 0) {
       if constexpr (ST > 1) {
         fetch(stage == 0 ? ST - 1 : stage - 1, next);
         next = look();
       }
-      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+      const bool ok = arrived(stage, phase);
       __syncwarp();
-      const uint32_t mask = s_mask[warp][stage];
+      const uint32_t mask = ok ? s_mask[warp][stage] : 0u;
+      if constexpr (LOAD == kDpEngine) {
+        constexpr uint32_t kAll = TK == 32 ? 0xffffffffu : (1u << TK) - 1u;
+        if (mask != 0u && mask != kAll) {  // zeros for the values that are not the request's: whatever lies there has weight 0, but may be NaN
+          constexpr int kChunks = E::RowBytes / 16, kPart = kChunks < 8 ? kChunks : 8;  // of a row, of a part of a row
+          const int32_t there = __popc(mask);
+          for (int32_t x = lane; x < (TK - there) * kChunks; x += 32) {
+            const int32_t row = there + x / kChunks, c = x % kChunks;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (uint32_t)stage * kStage + TK * E::KS + (c / kPart) * (TK * 128) + row * (kPart * 16) + (c % kPart) * 16), "r"(0) : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the copy engine writes there again
+          __syncwarp();
+        }
+      }
       if (mask) e.trip(ring + (uint32_t)stage * kStage, mask, s_e, warp);
       __syncwarp();  // every lane has read the stage before the next fetch overwrites it
-      end_of_request = ++tile == tiles_of(n);
-      end_of_run = i + 1 == total;
+      --run.left;
+      ++run.at;
+      end_of_request = ++run.tile == tiles_of(run.n);
       if constexpr (ST == 1) {
-        if (!end_of_run && !end_of_request) {
+        static_assert(CLUSTER, "one stage: nothing is loaded across the ends of requests");
+        if (run.left > 0) {
           fetch(0, next);
           next = look();
         }
       }
-      if (!end_of_request && !end_of_run) {
+      if (!end_of_request && run.left > 0) {
         stage = stage + 1 == ST ? 0 : stage + 1;
+        phase ^= stage == 0;
         continue;
       }
-    } else if (!CLUSTER) {
-      break;  // a run without tiles
     }
 
     // ---- the warps' results side by side, each over the stage that its warp has just used up
     e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
-    const int32_t r_done = r, h0_done = h0, nh_done = nh, g_done = g, vh_done = vh, n_done = n;
-    if (!CLUSTER && !end_of_run) {  // the next request's queries, while this one's results are joined
-      next_request(r, vh, n);
-      tile = 0;
-      heads_at(vh, g, h0, nh);
-      e.load(a, s_e, r, g, h0, nh);
+    const DpRun done = run;
+    const int32_t h0_done = h0, nh_done = nh, g_done = g;
+    bool more = false;
+    if constexpr (!CLUSTER) {  // the next request's queries, while this one's results are joined
+      if (run.left > 0) {
+        next_request(run.r, run.n);
+        run.tile = 0;
+        more = true;
+      } else if (c_runs < f_runs) {
+        __syncwarp();
+        run = s_run[warp][c_runs++ % kDpSteals];
+        more = true;
+      }
+      if (more) {
+        heads_at(run.vh, g, h0, nh);
+        e.load(a, s_e, run.r, g, h0, nh);
+      }
     }
     __syncthreads();
     if constexpr (CLUSTER) {
@@ -753,7 +918,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const bool whole = CLUSTER ? C == 1 : from_start && end_of_request;
     const int32_t cols = D / C;  // columns of every head that each CTA of the cluster finishes
     float* slot = nullptr;
-    if constexpr (!CLUSTER) slot = a.part + (2 * (int64_t)blockIdx.x + (from_start ? 1 : 0)) * dp_part_floats<E>();
+    if constexpr (!CLUSTER) slot = a.part + (2 * (int64_t)done.id + (from_start ? 1 : 0)) * dp_part_floats<E>();
     for (int32_t x = tid; x < nh_done * (D / 4); x += kThreads) {  // one thread per four columns of a head
       const int32_t h = x / (D / 4), col = 4 * (x % (D / 4));
       float top = -INFINITY;
@@ -770,10 +935,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         l = fmaf(wgt, s_ml[w][h][1], l);
       }
       if (whole) {
-        const int64_t hq = (int64_t)r_done * a.n_q_heads + h0_done + h;
-        const float inv = n_done > 0 ? vs / l : 0.f;
+        const int64_t hq = (int64_t)done.r * a.n_q_heads + h0_done + h;
+        const float inv = done.n > 0 ? vs / l : 0.f;
         dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + col, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-        if (col == 0 && a.lse) a.lse[hq] = n_done > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (col == 0 && a.lse) a.lse[hq] = done.n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
       } else if constexpr (CLUSTER) {
         const uint32_t to = (uint32_t)(col / cols);
         asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec_mapa(s_part + (rank * nh_done + h) * cols + col % cols, to)),
@@ -791,17 +956,23 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if constexpr (CLUSTER) {
       break;
     } else {
-      if (from_start && !end_of_request && tid == 0) {  // the first of several parts: the one that holds the request's last tile is
-        const int64_t last = first + i + (tiles_of(n_done) - tile);  // tile `last` of all, in run (last + 1) runs - 1 over all
-        const int32_t until = (int32_t)(((last + 1) * runs - 1) / all);
-        reinterpret_cast<ChainRecord*>(a.chains)[blockIdx.x] = {r_done, vh_done, until - (int32_t)blockIdx.x + 1, 0};
+      if (from_start && !end_of_request && tid == 0) {  // the first of several parts; the last is the run with the request's last tile
+        const int64_t last = done.at - 1 + (tiles_of(done.n) - done.tile);
+        const int32_t j = done.id / a.v_heads;
+        const int32_t until = (int32_t)(last < a.n_long * long_tiles ? last / long_tiles : a.n_long + (last - a.n_long * long_tiles) / short_tiles);
+        chains[done.id] = {done.r, done.vh, until - j + 1, 0};
       }
-      if (end_of_run) break;
+      if (!more) break;
       e.ready(s_e);
+      if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again
       __syncthreads();
-      from_start = true;
+      from_start = run.tile == 0;
       stage = stage + 1 == ST ? 0 : stage + 1;
+      phase ^= stage == 0;
     }
+  }
+  if constexpr (!CLUSTER) {
+    if (f_empty && tid == 0) drain(f_answers);
   }
 
   if constexpr (CLUSTER) {
@@ -837,35 +1008,55 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       acc += __shfl_xor_sync(0xffffffffu, acc, 2);
       l += __shfl_xor_sync(0xffffffffu, l, 2);
       if (part == 0 && x < nh * cols * 4) {
-        const int64_t hq = (int64_t)r * a.n_q_heads + h0 + h;
-        reinterpret_cast<Out*>(a.o)[hq * D + rank * cols + c] = (Out)(n > 0 ? acc * (vs / l) : 0.f);
-        if (rank == 0 && c == 0 && a.lse) a.lse[hq] = n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        const int64_t hq = (int64_t)run.r * a.n_q_heads + h0 + h;
+        reinterpret_cast<Out*>(a.o)[hq * D + rank * cols + c] = (Out)(run.n > 0 ? acc * (vs / l) : 0.f);
+        if (rank == 0 && c == 0 && a.lse) a.lse[hq] = run.n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
     }
   }
 }
 
-// Joins the parts of the requests that cuts went through: grid (half of the balanced form's CTAs, heads of a tile), a block looks
-// after two CTAs' chains.  Each D / 4 threads take eight parts at a time, all loads of which are asked for before the first is used, and
-// run a softmax of their own over them; the groups meet in shared memory.
-template <class E>
+// Joins the parts of the requests that cuts went through: grid (runs / J, heads of a tile / HPB).  A block looks after J runs' chains, one
+// after the other, and HPB heads of each: D / 4 threads per head, and as many groups of those as 256 threads hold.  A group takes eight or
+// sixteen parts at a time, all loads of which are asked for before the first is used, and runs a softmax of its own over them; the groups meet in
+// shared memory.  Many chains of few parts: a block each, all heads (J 1, HPB 8).  Few chains, of many parts: a head each (J 8, HPB 1).
+// Requests without rows get their zeros here.
+template <class E, int HPB, int J>
 __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
-  constexpr int D = E::D, R = E::R, kGroup = D / 4, kGroups = 256 / kGroup, kAtOnce = 8;
-  __shared__ float s_ml[kGroups][2];
+  constexpr int D = E::D, R = E::R, kHead = D / 4, kGroup = HPB * kHead, kGroups = 256 / kGroup, kAtOnce = J == 1 ? 16 : 8;
+  static_assert(kGroups >= 1, "a head's columns fit a block");
+  using Out = typename E::Out;
+  __shared__ float s_ml[kGroups][HPB][2];
   __shared__ __align__(16) float4 s_acc[kGroups][kGroup];
-  const int32_t h = blockIdx.y, grp = threadIdx.x / kGroup, c = threadIdx.x % kGroup;
+  const int32_t grp = threadIdx.x / kGroup, in_grp = threadIdx.x % kGroup, hb = in_grp / kHead, c = in_grp % kHead, h = blockIdx.y * HPB + hb;
+  const int32_t runs = a.v_heads * (a.n_long + a.n_short);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const ChainRecord both[2] = {reinterpret_cast<const ChainRecord*>(a.chains)[2 * blockIdx.x], reinterpret_cast<const ChainRecord*>(a.chains)[2 * blockIdx.x + 1]};
+  ChainRecord chains[J];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const ChainRecord chain = both[which];
-    const int32_t g = a.blocks == 1 ? chain.vh : chain.vh / a.blocks, b = chain.vh - g * a.blocks;
-    if (chain.parts == 0 || h >= min(R, a.group - b * R)) continue;  // the same for the block
-    const int64_t cta = 2 * blockIdx.x + which;
+  for (int k = 0; k < J; ++k) {
+    const int32_t b = blockIdx.x + k * gridDim.x;  // (neighbours begin the same request for different heads)
+    chains[k] = b < runs ? reinterpret_cast<const ChainRecord*>(a.chains)[b] : ChainRecord{};
+  }
+  for (int32_t r = blockIdx.x; r < a.n_req; r += gridDim.x) {
+    const int32_t len = a.view.seq_lens[r];
+    if (len > a.view.capacity() && blockIdx.y == 0 && threadIdx.x == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+    if (min(len, a.view.capacity()) > 0) continue;
+    for (int32_t hq = h; hq < a.n_q_heads; hq += gridDim.y * HPB)
+      if (grp == 0) {
+        dp_store4(reinterpret_cast<Out*>(a.o) + ((int64_t)r * a.n_q_heads + hq) * D + 4 * c, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (c == 0 && a.lse) a.lse[(int64_t)r * a.n_q_heads + hq] = -INFINITY;
+      }
+  }
+#pragma unroll
+  for (int which = 0; which < J; ++which) {
+    const ChainRecord chain = chains[which];
+    const int32_t g = a.blocks == 1 ? chain.vh : chain.vh / a.blocks, b = chain.vh - g * a.blocks, nh = min(R, a.group - b * R);
+    if (chain.parts == 0) continue;  // the same for the block
+    const int64_t first = blockIdx.x + (int64_t)which * gridDim.x;
     float ref = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int32_t i0 = grp; i0 < chain.parts; i0 += kAtOnce * kGroups) {
+    for (int32_t i0 = grp; i0 < chain.parts && h < nh; i0 += kAtOnce * kGroups) {
       float mi[kAtOnce], li[kAtOnce];
       float4 v[kAtOnce];
 #pragma unroll
@@ -875,7 +1066,7 @@ __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_con
         li[k] = 0.f;
         v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i < chain.parts) {
-          const float* slot = a.part + (2 * (cta + i) + (i == 0 ? 1 : 0)) * dp_part_floats<E>();
+          const float* slot = a.part + (2 * (first + (int64_t)i * a.v_heads) + (i == 0 ? 1 : 0)) * dp_part_floats<E>();
           mi[k] = slot[R * D + h];
           li[k] = slot[R * D + R + h];
           v[k] = *reinterpret_cast<const float4*>(slot + h * D + 4 * c);
@@ -895,32 +1086,34 @@ __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_con
         acc.x = fmaf(w, v[k].x, acc.x); acc.y = fmaf(w, v[k].y, acc.y); acc.z = fmaf(w, v[k].z, acc.z); acc.w = fmaf(w, v[k].w, acc.w);
       }
     }
-    if (c == 0) {
-      s_ml[grp][0] = ref;
-      s_ml[grp][1] = l;
-    }
-    s_acc[grp][c] = acc;
-    __syncthreads();
-    if (grp == 0) {
+    if constexpr (kGroups > 1) {
+      if (c == 0) {
+        s_ml[grp][hb][0] = ref;
+        s_ml[grp][hb][1] = l;
+      }
+      s_acc[grp][in_grp] = acc;
+      __syncthreads();
       float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) top = fmaxf(top, dp_seen(s_ml[i][0], s_ml[i][1]));
-      const float to = dp_finite(top);
+      for (int i = 0; i < kGroups; ++i) top = fmaxf(top, dp_seen(s_ml[i][hb][0], s_ml[i][hb][1]));
+      ref = dp_finite(top);
       acc = make_float4(0.f, 0.f, 0.f, 0.f);
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        const float w = dp_weight(s_ml[i][0], s_ml[i][1], to);
-        const float4 v = s_acc[i][c];
-        l = fmaf(w, s_ml[i][1], l);
+        const float w = dp_weight(s_ml[i][hb][0], s_ml[i][hb][1], ref);
+        const float4 v = s_acc[i][in_grp];
+        l = fmaf(w, s_ml[i][hb][1], l);
         acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
       }
+      __syncthreads();
+    }
+    if (grp == 0 && h < nh) {
       const int64_t hq = (int64_t)chain.r * a.n_q_heads + g * a.group + b * R + h;
       const float inv = (a.v_scale ? a.v_scale[g] : 1.f) / l;
-      dp_store4(reinterpret_cast<typename E::Out*>(a.o) + hq * D + 4 * c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (c == 0 && a.lse) a.lse[hq] = (to + log2f(l)) * 0.6931471805599453f;
+      dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + 4 * c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      if (c == 0 && a.lse) a.lse[hq] = (dp_finite(ref) + log2f(l)) * 0.6931471805599453f;
     }
-    __syncthreads();
   }
 }
 
@@ -942,9 +1135,9 @@ struct DpLaunch {
   }
 };
 
-template <class E, int W, int ST, bool WHOLE, int OCC>
+template <class E, int W, int ST, DpLoad LOAD, int OCC>
 static purekv_status launch_even(const DecodePagedArgs& a, int32_t cl, cudaStream_t stream) {
-  auto kernel = decode_paged_kernel<E, W, ST, true, WHOLE, OCC>;
+  auto kernel = decode_paged_kernel<E, W, ST, true, LOAD, OCC>;
   static std::atomic<uint64_t> smem_allowed{0}, wide_allowed{0};
   const purekv_status st = allow_max_dynamic_smem(kernel, smem_allowed);
   if (st != PUREKV_OK) return st;
@@ -966,50 +1159,83 @@ static purekv_status launch_even(const DecodePagedArgs& a, int32_t cl, cudaStrea
     set_size(c);
     return clusters_at_once(kernel, l.cfg);
   }));
-  PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a));
+  PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a, DpMaps{}));
   return PUREKV_OK;
 }
 
-template <class E, int W, int ST, bool WHOLE, int OCC>
-static purekv_status launch_balanced(const DecodePagedArgs& a, int32_t ctas, cudaStream_t stream) {
-  auto kernel = decode_paged_kernel<E, W, ST, false, WHOLE, OCC>;
+template <class E, int W, int ST, DpLoad LOAD, int OCC>
+static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& maps, cudaStream_t stream) {
+  auto kernel = decode_paged_kernel<E, W, ST, false, LOAD, OCC>;
   static std::atomic<uint64_t> smem_allowed{0};
   const purekv_status st = allow_max_dynamic_smem(kernel, smem_allowed);
   if (st != PUREKV_OK) return st;
-  DpLaunch l(dim3((unsigned)ctas), W * 32, (size_t)W * dp_warp_bytes<E, ST>(), stream);
-  PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a));
-  DpLaunch j(dim3((unsigned)(ctas / 2), (unsigned)std::min(E::R, a.group)), 256, 0, stream);
-  PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E>, a));
+  const int32_t runs = a.v_heads * (a.n_long + a.n_short);
+  DpLaunch l(dim3((unsigned)runs), W * 32, (size_t)W * dp_warp_bytes<E, ST>() + (LOAD == kDpEngine ? 1024 : 0), stream);
+  PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a, maps));
+  // (segments that cuts can go through: requests x heads; 16 parts each on average at the limit)
+  constexpr int kWide = E::R < 8 ? E::R : 8;
+  const bool many = (int64_t)a.n_req * a.v_heads * 16 >= runs;
+  const int32_t heads = std::min(E::R, a.group);
+  DpLaunch j(many ? dim3((unsigned)runs, (unsigned)((heads + kWide - 1) / kWide)) : dim3((unsigned)((runs + 7) / 8), (unsigned)heads), 256, 0, stream);
+  if (many)
+    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E, kWide, 1>, a));
+  else
+    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E, 1, 8>, a));
   return PUREKV_OK;
 }
 
-constexpr int32_t kDpCtas = 296;  // CTAs of the balanced form: two per SM
-
-// How a call is launched: C CTAs per (request, head) in a cluster, or 0 for the balanced form.
+// How a call is launched: C CTAs per (request, head) in a cluster, or, with 0, the balanced form with so many long and short runs of a
+// head.
 struct DpForm {
-  int32_t cluster;
+  int32_t cluster, at_once, n_long, n_short;
 };
-static DpForm dp_form(int64_t base, int64_t bound) {
+static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t bound) {
+  const int64_t base = n_req * v_heads;
   int32_t c = 1;
   while (c < kDpClusterMax && bound > 128 * c && base * 2 * c <= (c < 4 ? 128 : 64)) c *= 2;
-  return {bound <= 128 * (int64_t)c * 2 ? c : 0};
+  if (bound <= 128 * (int64_t)c * 2) return {c, 0, 0, 0};
+  const int32_t at_once = kDpAtOnce, shorts = kDpShorts * at_once;
+  return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((shorts + v_heads - 1) / v_heads)};
 }
 
-template <class E, int ST8, bool WHOLE>
-static purekv_status launch_form(const DecodePagedArgs& a, const DpForm& f, cudaStream_t stream) {
-  if (f.cluster) return launch_even<E, 8, ST8, WHOLE, 1>(a, f.cluster, stream);
-  return launch_balanced<E, 4, ST8, WHOLE, 2>(a, kDpCtas, stream);
+// The pools for the copy engine; false where it cannot take them.
+template <class E>
+static bool dp_maps(const DecodePagedArgs& a, int32_t n_kv_heads, DpMaps* maps) {
+  const tc::EncodeTiledFn encode = tc::encode_fn();
+  if (!encode) return false;
+  constexpr cuuint32_t kInner = E::RowBytes < 128 ? E::RowBytes : 128, kParts = E::RowBytes / kInner;
+  auto stride = [](int64_t s) { return (cuuint64_t)(s > 0 ? s : E::RowBytes); };  // (0: a dimension of size 1)
+  const cuuint64_t dims[5] = {kInner, (cuuint64_t)a.view.page_size.d, kParts, (cuuint64_t)n_kv_heads, (cuuint64_t)a.view.n_pages};
+  const cuuint64_t strides[4] = {stride(a.view.token_stride), 128, stride(a.view.head_stride), stride(a.view.page_stride)};
+  const cuuint32_t box[5] = {kInner, (cuuint32_t)E::TK, kParts, 1, 1}, each[5] = {1, 1, 1, 1, 1};
+  const uint8_t* pools[2] = {a.k_pool, a.v_pool};
+  CUtensorMap* out[2] = {&maps->k, &maps->v};
+  for (int i = 0; i < 2; ++i)
+    if (encode(out[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<uint8_t*>(pools[i]), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               kInner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+               kParts > 1 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : kInner == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  return true;
 }
-template <class E, int ST8>
-static purekv_status launch_rows(const DecodePagedArgs& a, const DpForm& f, cudaStream_t stream) {
-  return a.view.page_size.d % E::TK == 0 ? launch_form<E, ST8, true>(a, f, stream) : launch_form<E, ST8, false>(a, f, stream);
+
+// E: the engine for rows copied by threads; X: the same for rows that the copy engine brings.  ST8 and ST4: stages of each warp with
+// eight warps in a CTA and with two CTAs of four.
+template <class E, class X, int ST8, int ST4>
+static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
+  const bool whole = a.view.page_size.d % E::TK == 0 && a.view.n_pages > 0;
+  if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
+  DpMaps maps = {};
+  if (whole && dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, 2>(a, maps, stream);
+  return launch_balanced<E, 4, ST8, kDpRows, 2>(a, maps, stream);
 }
 
 static int32_t dp_rows(int32_t group, purekv_dtype dtype) { return dtype == PUREKV_FP32 ? (group <= 2 ? 2 : 8) : group <= 8 ? 8 : 16; }
 
-static int64_t dp_ws(const DpForm& f, int32_t group, int32_t head_dim, purekv_dtype dtype) {
+static int64_t dp_ws(const DpForm& f, int64_t v_heads, int32_t group, int32_t head_dim, purekv_dtype dtype) {
   if (f.cluster) return 0;
-  return 256 + kDpCtas * (int64_t)sizeof(ChainRecord) + 2 * kDpCtas * (int64_t)dp_rows(group, dtype) * (head_dim + 2) * 4;
+  const int64_t runs = v_heads * (f.n_long + f.n_short);
+  return 256 + runs * (int64_t)sizeof(ChainRecord) + 2 * runs * dp_rows(group, dtype) * (head_dim + 2) * 4;
 }
 
 }  // namespace purekv
@@ -1022,7 +1248,8 @@ size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_
                                     purekv_dtype dtype) {
   if (n_req <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || head_dim <= 0) return 0;
   const int32_t group = n_q_heads / n_kv_heads, rows = dp_rows(group, dtype), blocks = (group + rows - 1) / rows;
-  return (size_t)dp_ws(dp_form((int64_t)n_req * n_kv_heads * blocks, max_len > 0 ? max_len : INT32_MAX), group, head_dim, dtype);
+  const int64_t v_heads = (int64_t)n_kv_heads * blocks;
+  return (size_t)dp_ws(dp_form(n_req, v_heads, max_len > 0 ? max_len : INT32_MAX), v_heads, group, head_dim, dtype);
 }
 
 purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t q_head_stride, void* o, float* lse,
@@ -1064,12 +1291,16 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   a.o = o;
   a.lse = lse;
   a.status = status;
-  const DpForm form = dp_form((int64_t)a.n_req * a.v_heads, max_len > 0 ? max_len : INT32_MAX);
+  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX);
   if (!form.cluster) {
-    PK_REQUIRE(ws && ws_bytes >= (size_t)dp_ws(form, a.group, pages->head_dim, dtype), PUREKV_ERR_WORKSPACE,
+    PK_REQUIRE(ws && ws_bytes >= (size_t)dp_ws(form, a.v_heads, a.group, pages->head_dim, dtype), PUREKV_ERR_WORKSPACE,
                "%s: workspace of %zu bytes is too small", kName, ws_bytes);
     a.chains = (int32_t*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
-    a.part = (float*)(a.chains + kDpCtas * (sizeof(ChainRecord) / 4));
+    a.at_once = form.at_once;
+    a.n_long = form.n_long;
+    a.n_short = form.n_short;
+    a.wait_ns = wait_limit_ns();
+    a.part = (float*)(a.chains + (int64_t)a.v_heads * (a.n_long + a.n_short) * (sizeof(ChainRecord) / 4));
   }
   if (!status) {
     const purekv_status s2 = default_status_word(&a.status);
@@ -1077,16 +1308,18 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   }
   cudaStream_t sm = (cudaStream_t)stream;
   const bool wide = pages->head_dim == 128;
+#define PK_ROWS(ENGINE, D, N, ST8, ST4) launch_rows<ENGINE<D, N, false>, ENGINE<D, N, true>, ST8, ST4>(a, pages->n_kv_heads, form, sm)
   if (dtype == PUREKV_FP32) {
-    if (rows == 2) return wide ? launch_rows<Fp32Rows<128, 2>, 3>(a, form, sm) : launch_rows<Fp32Rows<64, 2>, 3>(a, form, sm);
-    return wide ? launch_rows<Fp32Rows<128, 8>, 3>(a, form, sm) : launch_rows<Fp32Rows<64, 8>, 3>(a, form, sm);
+    if (rows == 2) return wide ? PK_ROWS(Fp32Rows, 128, 2, 3, 3) : PK_ROWS(Fp32Rows, 64, 2, 3, 3);
+    return wide ? PK_ROWS(Fp32Rows, 128, 8, 3, 3) : PK_ROWS(Fp32Rows, 64, 8, 3, 3);
   }
   if (pages->dtype == PUREKV_E4M3) {
-    if (rows == 8) return wide ? launch_rows<E4m3Rows<128, 1>, 3>(a, form, sm) : launch_rows<E4m3Rows<64, 1>, 5>(a, form, sm);
-    return wide ? launch_rows<E4m3Rows<128, 2>, 2>(a, form, sm) : launch_rows<E4m3Rows<64, 2>, 5>(a, form, sm);
+    if (rows == 8) return wide ? PK_ROWS(E4m3Rows, 128, 1, 3, 3) : PK_ROWS(E4m3Rows, 64, 1, 5, 6);
+    return wide ? PK_ROWS(E4m3Rows, 128, 2, 2, 3) : PK_ROWS(E4m3Rows, 64, 2, 5, 6);
   }
-  if (rows == 8) return wide ? launch_rows<Bf16Rows<128, 1>, 3>(a, form, sm) : launch_rows<Bf16Rows<64, 1>, 5>(a, form, sm);
-  return wide ? launch_rows<Bf16Rows<128, 2>, 3>(a, form, sm) : launch_rows<Bf16Rows<64, 2>, 5>(a, form, sm);
+  if (rows == 8) return wide ? PK_ROWS(Bf16Rows, 128, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 1, 5, 6);
+  return wide ? PK_ROWS(Bf16Rows, 128, 2, 3, 3) : PK_ROWS(Bf16Rows, 64, 2, 5, 6);
+#undef PK_ROWS
 }
 
 }  // extern "C"
