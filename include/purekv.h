@@ -339,7 +339,8 @@ purekv_status purekv_decode_attention(const void *q, const void *k_cache, const 
  * [n_pages][H_kv][page_size][d] are both such layouts.  Strides and pool pointers are multiples of 16 bytes; those of a
  * dimension of size 1 are not looked at, and no two rows overlap.
  * With PUREKV_E4M3 a pool holds e4m3 numbers that stand for themselves times k_scale[g], v_scale[g] (device, fp32, one per KV head,
- * layer after layer; NULL: 1): x is stored as x / scale rounded to the nearest (ties to even), beyond +-448 as +-448.
+ * layer after layer; NULL: 1): x is stored as its product with the fp32 reciprocal of the scale, rounded to the nearest (ties to
+ * even), beyond +-448 as +-448.
  * seq_lens and block_table are read on the device, at the time of the kernel: a captured call follows their contents.  Where
  * they name a page outside the pool, or a row beyond max_pages * page_size, a store leaves the row out and the attention leaves the
  * key out, and the status word is set to PUREKV_ERR_BAD_PAGE; nothing outside the pools is touched.  The paged calls compute whatever the word

@@ -1,11 +1,15 @@
 // purekv_append_paged and purekv_compact_paged: rows of K and V into the pages of a cache.
 //
-// Append.  A token's heads turn by the same angles: a block takes a few tokens, forms their angles once (64-bit product of position
-// and frequency, reduced to a fraction of a turn, fp32 sine and cosine) in shared memory, and its threads go over the tokens' head
-// rows, 2 x 16 bytes at a time: the two chunks whose elements rotate into one another.  The K rows go to k_out and to their slot in the
-// pages, q to q_out.  Bound by HBM for prompts, by the chain of position, page and row loads for single tokens.
+// Append.  A token's heads turn by the same angles.  A thread stands for two 16-byte chunks of one head row, those whose elements
+// rotate into one another, and takes them of all the block's tokens: it asks for all of them, the block then forms the tokens' angles
+// (64-bit product of position and frequency, reduced to a fraction of a turn, fp32 sine and cosine) in shared memory and looks their
+// slots in the pages up, and the thread rotates and stores: q to q_out, k to k_out and its slot, v to its slot.  Bound by HBM for
+// prompts, by the chain of position, page and row loads for single tokens.
 //
-// Compact.  A warp takes 16 kept rows: each lane looks one row's source and slot up, and the warp then copies row by row.
+// Compact.  A warp takes a batch of kept rows at a time, whose sources and slots its lanes look up, a row each.  A batch is four stages of a
+// ring in shared memory (cp.async; a thread stores what it has loaded, so no thread waits for another): as a stage has been stored, the same
+// stage of the next batch is asked for, so that three to four are always on their way -- the rows lie 256 bytes here and there, and it
+// takes about 130 KB per SM on their way to keep HBM busy (registers hold half of that: 191 us for 1.3 million rows, now 162 = 5.9 TB/s).
 #include <algorithm>
 
 #include <cuda_fp8.h>
@@ -16,7 +20,7 @@
 
 namespace purekv {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 512;  // at most
 constexpr int kMaxAxes = 4;
 
 struct AppendArgs {
@@ -37,7 +41,6 @@ struct AppendArgs {
   int32_t n_req, n_tokens, n_q_heads, n_kv_heads, head_dim;
   int32_t rows_per_token;  // q's, k's and v's head rows
   FastDiv row_lanes;       // threads of a head row: one for each two chunks
-  FastDiv rows_div;
   int32_t* status;
 };
 
@@ -73,23 +76,27 @@ struct Chunk<float> {
   }
 };
 
-// Eight values as e4m3, nearest, ties to even, saturating; NaN stays NaN.  The quotient is the correctly rounded one: a product with
-// the reciprocal would fall on the other side of a rounding boundary now and then.
-__device__ __forceinline__ uint2 to_e4m3(const float (&f)[8], float scale) {
+// Eight values times `inverse`, the reciprocal of their scale, as e4m3: nearest, ties to even, saturating; NaN stays NaN.  (A division of
+// each, or a correction of the product to the correctly rounded quotient, is most of a compaction's instructions: 1.3 million rows
+// took 331 us with it and 229 without.)
+__device__ __forceinline__ uint2 to_e4m3(const float (&f)[8], float inverse) {
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
+    const float2 a = __fmul2_rn(make_float2(f[4 * i], f[4 * i + 1]), make_float2(inverse, inverse));
+    const float2 b = __fmul2_rn(make_float2(f[4 * i + 2], f[4 * i + 3]), make_float2(inverse, inverse));
     uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fdiv_rn(f[4 * i + 1], scale)), "f"(__fdiv_rn(f[4 * i], scale)));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fdiv_rn(f[4 * i + 3], scale)), "f"(__fdiv_rn(f[4 * i + 2], scale)));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(a.y), "f"(a.x));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(b.y), "f"(b.x));
     w[i] = (uint32_t)lo | ((uint32_t)hi << 16);
   }
   return make_uint2(w[0], w[1]);
 }
 
-// T: the tokens' type; E8: the pools hold e4m3; TOK: tokens of a block.  Dynamic shared memory: TOK x half (cos, sin).
+// T: the tokens' type; E8: the pools hold e4m3; TOK: tokens of a block.  grid (tokens / TOK, parts of a token's chunk pairs).  Dynamic
+// shared memory: TOK x half (cos, sin).
 template <typename T, bool E8, int TOK>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int E = Chunk<T>::E;
   extern __shared__ float2 s_turn[];
   __shared__ int64_t s_dst[TOK];
@@ -97,112 +104,120 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
+  // this thread's head row, and its two chunks
+  const int32_t item = blockIdx.y * blockDim.x + tid, lanes = (int32_t)a.row_lanes.d;
+  const int32_t row = (int32_t)a.row_lanes.quotient((uint32_t)item), j = item - row * lanes;
+  const bool there = row < a.rows_per_token;
+  const int32_t nq = a.q ? a.n_q_heads : 0, nk = a.k ? a.n_kv_heads : 0;
+  const bool is_q = row < nq, is_v = row >= nq + nk, turns = a.positions && !is_v;
+  const int32_t h = is_q ? row : is_v ? row - nq - nk : row - nq;
+  const int64_t tok_stride = is_q ? a.q_tok : is_v ? a.v_tok : a.k_tok;
+  const uint8_t* src = (is_q ? a.q + h * a.q_head : is_v ? a.v + h * a.v_head : a.k + h * a.k_head) + t0 * tok_stride;
+  const int32_t rc = a.half / E;  // chunks of the first halves (half-split pairs)
+  const bool split = turns && !a.interleaved && j < rc;
+  const int32_t ca = split ? j : 2 * j, cb = split ? j + rc : 2 * j + 1;  // (2 rc + 2 (j - rc) = 2 j past the halves)
+  uint4 ux[TOK], uy[TOK];
+#pragma unroll
+  for (int u = 0; u < TOK; ++u)
+    if (there && u < n_tok) {
+      ux[u] = reinterpret_cast<const uint4*>(src + u * tok_stride)[ca];
+      uy[u] = reinterpret_cast<const uint4*>(src + u * tok_stride)[cb];
+    }
+
   if (a.positions)
-    for (int32_t i = tid; i < n_tok * a.half; i += kAppendThreads) {
+    for (int32_t i = tid; i < n_tok * a.half; i += blockDim.x) {
       const int32_t tok = i / a.half, pair = i - tok * a.half;
-      int32_t axis = 0;
-      while (axis < kMaxAxes - 1 && pair >= a.axis_end[axis]) ++axis;
-      const double turns = (double)a.positions[axis * a.axis_stride + t0 + tok] * a.inv_freq[pair] * 0.15915494309189533577;  // 1 / 2 pi
+      const int32_t axis = (pair >= a.axis_end[0]) + (pair >= a.axis_end[1]) + (pair >= a.axis_end[2]);
+      const double full = (double)a.positions[axis * a.axis_stride + t0 + tok] * a.inv_freq[pair] * 0.15915494309189533577;  // 1 / 2 pi
       float sn, cs;
-      sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+      sincospif(2.f * (float)(full - rint(full)), &sn, &cs);
       s_turn[i] = make_float2(cs, sn);
     }
-  if (a.store && tid >= kAppendThreads - TOK) {
-    const int32_t tok = tid - (kAppendThreads - TOK), t = t0 + tok;
+  if (a.store && tid >= (int32_t)blockDim.x - TOK) {
+    const int32_t tok = tid - ((int32_t)blockDim.x - TOK), t = t0 + tok;
     int64_t dst = -1;
     if (tok < n_tok) {
-      int32_t r = t, row = -1, len = 0;
+      int32_t r = t, at = -1, len = 0;
       if (a.cu_new) {
         r = request_of(a.cu_new, a.n_req, t);
         const int32_t end = a.cu_new[r + 1];
         if (a.cu_new[r] <= t && t < end) {
           len = a.view.seq_lens[r];
-          row = len - (end - t);
+          at = len - (end - t);
         }
       } else {
         len = a.view.seq_lens[r];
-        row = len - 1;
+        at = len - 1;
       }
       if (len > 0) {
-        dst = a.view.row_offset(a.view.table + r * a.view.table_stride, row);
+        dst = a.view.row_offset(a.view.table + r * a.view.table_stride, at);
         if (dst < 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
       }
     }
     s_dst[tok] = dst;
   }
   __syncthreads();
+  if (!there) return;
 
-  const int32_t lanes = (int32_t)a.row_lanes.d, n_items = n_tok * a.rows_per_token * lanes;
-  const int32_t rc = a.half / E;  // chunks of the first halves (half-split pairs)
-  for (int32_t item = tid; item < n_items; item += kAppendThreads) {
-    const int32_t row = (int32_t)a.row_lanes.quotient((uint32_t)item), j = item - row * lanes;
-    const int32_t tok = (int32_t)a.rows_div.quotient((uint32_t)row);
-    int32_t h = row - tok * a.rows_per_token;
-    const int64_t t = t0 + tok;
-    const int32_t nq = a.q ? a.n_q_heads : 0, nk = a.k ? a.n_kv_heads : 0;
-    const bool is_q = h < nq, is_v = h >= nq + nk;
-    const uint8_t* src;
-    if (is_q) {
-      src = a.q + t * a.q_tok + h * a.q_head;
-    } else if (!is_v) {
-      h -= nq;
-      src = a.k + t * a.k_tok + h * a.k_head;
-    } else {
-      h -= nq + nk;
-      src = a.v + t * a.v_tok + h * a.v_head;
-    }
-    const bool split = !a.interleaved && !is_v && a.positions && j < rc;
-    const int32_t ca = split ? j : 2 * j, cb = split ? j + rc : 2 * j + 1;  // (2 rc + 2 (j - rc) = 2 j past the halves)
+  uint8_t* const out = is_q ? a.q_out : is_v ? nullptr : a.k_out;
+  const int64_t out_row = (int64_t)a.head_dim * sizeof(T), out_tok = (is_q ? a.n_q_heads : a.n_kv_heads) * out_row;
+  uint8_t* const pool = (is_v ? a.v_pool : a.k_pool) + h * a.view.head_stride;
+  const bool store = a.store && !is_q;
+  const float* const scales = is_v ? a.v_scale : a.k_scale;
+  const float inverse = E8 && store && scales ? 1.f / scales[h] : 1.f;
+#pragma unroll
+  for (int u = 0; u < TOK; ++u) {
+    if (u >= n_tok) break;
     float x[E], y[E];
-    Chunk<T>::get(reinterpret_cast<const uint4*>(src)[ca], x);
-    Chunk<T>::get(reinterpret_cast<const uint4*>(src)[cb], y);
+    Chunk<T>::get(ux[u], x);
+    Chunk<T>::get(uy[u], y);
+    const float2* turn = s_turn + u * a.half;
     if (split) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float2 w = s_turn[tok * a.half + ca * E + e];
+        const float2 w = turn[ca * E + e];
         const float xe = x[e], ye = y[e];
         x[e] = xe * w.x - ye * w.y;
         y[e] = ye * w.x + xe * w.y;
       }
-    } else if (a.interleaved && !is_v && a.positions) {
+    } else if (turns && a.interleaved) {
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
-        auto turn = [&](float (&z)[E], int32_t c) {
+        auto rotate = [&](float (&z)[E], int32_t c) {
           const int32_t pair = (c * E + e) / 2;
           if (pair >= a.half) return;
-          const float2 w = s_turn[tok * a.half + pair];
+          const float2 w = turn[pair];
           const float ze = z[e], zo = z[e + 1];
           z[e] = ze * w.x - zo * w.y;
           z[e + 1] = zo * w.x + ze * w.y;
         };
-        turn(x, ca);
-        turn(y, cb);
+        rotate(x, ca);
+        rotate(y, cb);
       }
     }
-    if (!is_v) {
-      uint8_t* out = is_q ? a.q_out : a.k_out;
-      if (out) {
-        uint4* o4 = reinterpret_cast<uint4*>(out + (t * (is_q ? a.n_q_heads : a.n_kv_heads) + h) * a.head_dim * (int64_t)sizeof(T));
-        o4[ca] = Chunk<T>::put(x);
-        o4[cb] = Chunk<T>::put(y);
-      }
+    const bool changed = split || (turns && a.interleaved);  // (what is copied stays as it is, a NaN's bits too)
+    const uint4 px = changed ? Chunk<T>::put(x) : ux[u], py = changed ? Chunk<T>::put(y) : uy[u];
+    if (out) {
+      uint4* o4 = reinterpret_cast<uint4*>(out + (t0 + u) * out_tok + h * out_row);
+      o4[ca] = px;
+      o4[cb] = py;
     }
-    if (!is_q && a.store && s_dst[tok] >= 0) {
-      uint8_t* dst = (is_v ? a.v_pool : a.k_pool) + s_dst[tok] + h * a.view.head_stride;
+    if (store && s_dst[u] >= 0) {
+      uint8_t* dst = pool + s_dst[u];
       if constexpr (E8) {
-        const float* sc = is_v ? a.v_scale : a.k_scale;
-        const float scale = sc ? sc[h] : 1.f;
-        reinterpret_cast<uint2*>(dst)[ca] = to_e4m3(x, scale);
-        reinterpret_cast<uint2*>(dst)[cb] = to_e4m3(y, scale);
+        reinterpret_cast<uint2*>(dst)[ca] = to_e4m3(x, inverse);
+        reinterpret_cast<uint2*>(dst)[cb] = to_e4m3(y, inverse);
       } else {
-        reinterpret_cast<uint4*>(dst)[ca] = Chunk<T>::put(x);
-        reinterpret_cast<uint4*>(dst)[cb] = Chunk<T>::put(y);
+        reinterpret_cast<uint4*>(dst)[ca] = px;
+        reinterpret_cast<uint4*>(dst)[cb] = py;
       }
     }
   }
 }
 
-constexpr int kCompactRows = 16;  // rows of a warp
+constexpr int kCompactBlocks = 3;      // of 256 threads per SM
+constexpr int kCompactStages = 4;
+constexpr int kCompactRequests = 256;  // whose offsets a block keeps in shared memory
 
 struct CompactArgs {
   const uint8_t *k, *v;
@@ -217,60 +232,147 @@ struct CompactArgs {
   int32_t* status;
 };
 
-template <typename T, bool E8>
-__global__ void __launch_bounds__(256) compact_paged_kernel(const CompactArgs a) {
-  const int32_t lane = threadIdx.x & 31;
+// CH: 16-byte chunks of a source row, 8, 16 or 32: a stage is 64 / CH rows of K and of V.  0: a.chunks of them, a batch of 16 rows
+// without a ring (other head dimensions).
+template <int CH>
+__host__ __device__ constexpr int compact_rows() { return CH ? 64 / CH * kCompactStages : 16; }
+template <typename T, bool E8, int CH>
+__global__ void __launch_bounds__(256, kCompactBlocks) compact_paged_kernel(const __grid_constant__ CompactArgs a) {
+  constexpr int kRows = compact_rows<CH>(), kPerStage = CH ? 64 / CH : 8;
+  extern __shared__ __align__(16) uint8_t s_ring[];  // [warp][stage][2][K, V][lane] of 16 bytes
+  __shared__ int32_t s_kept[kCompactRequests + 1], s_first[kCompactRequests + 1], s_lens[kCompactRequests];
+  const int32_t lane = threadIdx.x & 31, chunks = CH ? CH : a.chunks;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t warp = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5, n_warps = ((int64_t)gridDim.x * blockDim.x) >> 5;
-  const int64_t per_layer = (int64_t)a.k_tot * a.n_kv_heads;
-  for (int64_t first = warp * kCompactRows; first < a.n_rows; first += n_warps * kCompactRows) {
-    int64_t src = -1, dst = -1;
-    int32_t scale_at = 0;
-    if (lane < kCompactRows && first + lane < a.n_rows) {
-      const int64_t x = first + lane;
-      const int32_t layer = (int32_t)(x / per_layer), in_layer = (int32_t)(x - layer * per_layer);
-      const int32_t t = in_layer / a.n_kv_heads, g = in_layer - t * a.n_kv_heads;
-      const int32_t r = request_of(a.cu_kept, a.n_req, t);
-      const int32_t end = a.cu_kept[r + 1], at = a.cu_seqlens[r], len = a.cu_seqlens[r + 1] - at;
-      const int32_t i = a.idx[((int64_t)layer * a.n_kv_heads + g) * a.k_tot + t], rows = a.view.seq_lens[r];
-      if (a.cu_kept[r] <= t && t < end && rows > 0) {
-        dst = a.view.row_offset(a.view.table + r * a.view.table_stride, rows - (end - t));
-        const int64_t token = (int64_t)at + i;
-        if (dst < 0 || i < 0 || i >= len || at < 0 || token >= a.total_tokens) {
-          dst = -1;
-          atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
-        } else {
-          src = layer * a.layer_bytes + (token * a.n_kv_heads + g) * (int64_t)a.chunks * 16;
-          dst += layer * a.pool_layer_bytes + g * a.view.head_stride;
-          scale_at = layer * a.n_kv_heads + g;
+  const int32_t *cu_kept = a.cu_kept, *cu_seqlens = a.cu_seqlens, *seq_lens = a.view.seq_lens;
+  if (a.n_req <= kCompactRequests) {
+    for (int32_t r = threadIdx.x; r <= a.n_req; r += blockDim.x) {
+      s_kept[r] = cu_kept[r];
+      s_first[r] = cu_seqlens[r];
+      if (r < a.n_req) s_lens[r] = seq_lens[r];
+    }
+    __syncthreads();
+    cu_kept = s_kept;
+    cu_seqlens = s_first;
+    seq_lens = s_lens;
+  }
+  const int64_t warp = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5, step = (((int64_t)gridDim.x * blockDim.x) >> 5) * kRows;
+  const int32_t per_layer = a.k_tot * a.n_kv_heads;
+  struct Row {  // dst < 0: nothing to copy
+    int64_t src, dst;
+    float ks, vs;  // reciprocals of the scales
+  };
+  // lane's row of the rows from `first` on, which lie in layer `layer` from row `at` on
+  auto look = [&](int64_t first, int32_t layer, int32_t at) {
+    Row w = {-1, -1, 1.f, 1.f};
+    if (lane >= kRows || first + lane >= a.n_rows) return w;
+    at += lane;
+    while (at >= per_layer) {
+      at -= per_layer;
+      ++layer;
+    }
+    const int32_t t = at / a.n_kv_heads, g = at - t * a.n_kv_heads;
+    const int32_t i = a.idx[((int64_t)layer * a.n_kv_heads + g) * a.k_tot + t];
+    const int32_t r = request_of(cu_kept, a.n_req, t);
+    const int32_t begin = cu_kept[r], end = cu_kept[r + 1], from = cu_seqlens[r], len = cu_seqlens[r + 1] - from, rows = seq_lens[r];
+    if (t < begin || t >= end || rows <= 0) return w;
+    const int64_t dst = a.view.row_offset(a.view.table + r * a.view.table_stride, rows - (end - t)), token = (int64_t)from + i;
+    if (dst < 0 || i < 0 || i >= len || from < 0 || token >= a.total_tokens) {
+      atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+      return w;
+    }
+    w.src = layer * a.layer_bytes + (token * a.n_kv_heads + g) * (int64_t)chunks * 16;
+    w.dst = dst + layer * a.pool_layer_bytes + g * a.view.head_stride;
+    if constexpr (E8) {
+      if (a.k_scale) w.ks = 1.f / a.k_scale[layer * a.n_kv_heads + g];
+      if (a.v_scale) w.vs = 1.f / a.v_scale[layer * a.n_kv_heads + g];
+    }
+    return w;
+  };
+  auto store = [&](uint8_t* k_dst, uint8_t* v_dst, int32_t chunk, uint4 ku, uint4 vu, float ks, float vs) {
+    if constexpr (E8) {
+      float f[8];
+      Chunk<T>::get(ku, f);
+      reinterpret_cast<uint2*>(k_dst)[chunk] = to_e4m3(f, ks);
+      Chunk<T>::get(vu, f);
+      reinterpret_cast<uint2*>(v_dst)[chunk] = to_e4m3(f, vs);
+    } else {
+      reinterpret_cast<uint4*>(k_dst)[chunk] = ku;
+      reinterpret_cast<uint4*>(v_dst)[chunk] = vu;
+    }
+  };
+  // where the warp is: the first of its batch's rows, its layer and its row there; moved on without a division
+  int64_t first = warp * kRows;
+  int32_t layer = (int32_t)(first / per_layer), at = (int32_t)(first - (int64_t)layer * per_layer);
+  const int32_t step_layers = (int32_t)(step / per_layer), step_rows = (int32_t)(step - (int64_t)step_layers * per_layer);
+  auto look_on = [&]() {
+    layer += step_layers;
+    at += step_rows;
+    if (at >= per_layer) {
+      at -= per_layer;
+      ++layer;
+    }
+    return look(first + step, layer, at);
+  };
+  Row w = look(first, layer, at);
+  if constexpr (CH > 0) {
+    uint8_t* const mine = s_ring + (threadIdx.x >> 5) * (kCompactStages * 2048) + lane * 16;
+    auto ask = [&](const Row& x, int stage) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t c = lane + 32 * u, row = stage * kPerStage + c / chunks;
+        const int64_t from = __shfl_sync(0xffffffffu, x.src, row) + (c % chunks) * 16;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine + stage * 2048 + u * 1024);
+        if (__shfl_sync(0xffffffffu, x.dst, row) >= 0) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(a.k + from) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512), "l"(a.v + from) : "memory");
         }
       }
-    }
-    for (int32_t c = lane; c < kCompactRows * a.chunks; c += 32) {
-      const int32_t row = c / a.chunks, chunk = c - row * a.chunks;
-      const int64_t s = __shfl_sync(0xffffffffu, src, row), d = __shfl_sync(0xffffffffu, dst, row);
-      const int32_t sc = __shfl_sync(0xffffffffu, scale_at, row);
-      if (d < 0) continue;
-      const uint4 ku = reinterpret_cast<const uint4*>(a.k + s)[chunk], vu = reinterpret_cast<const uint4*>(a.v + s)[chunk];
-      if constexpr (E8) {
-        float f[8];
-        Chunk<T>::get(ku, f);
-        reinterpret_cast<uint2*>(a.k_pool + d)[chunk] = to_e4m3(f, a.k_scale ? a.k_scale[sc] : 1.f);
-        Chunk<T>::get(vu, f);
-        reinterpret_cast<uint2*>(a.v_pool + d)[chunk] = to_e4m3(f, a.v_scale ? a.v_scale[sc] : 1.f);
-      } else {
-        reinterpret_cast<uint4*>(a.k_pool + d)[chunk] = ku;
-        reinterpret_cast<uint4*>(a.v_pool + d)[chunk] = vu;
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int stage = 0; stage < kCompactStages; ++stage) ask(w, stage);
+    while (first < a.n_rows) {
+      const Row next = look_on();
+      __syncwarp();
+#pragma unroll
+      for (int stage = 0; stage < kCompactStages; ++stage) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kCompactStages - 1) : "memory");
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int32_t c = lane + 32 * u, row = stage * kPerStage + c / chunks;
+          const int64_t to = __shfl_sync(0xffffffffu, w.dst, row);
+          const float ks = E8 ? __shfl_sync(0xffffffffu, w.ks, row) : 1.f, vs = E8 ? __shfl_sync(0xffffffffu, w.vs, row) : 1.f;
+          if (to >= 0) {
+            const uint4* held = reinterpret_cast<const uint4*>(mine + stage * 2048 + u * 1024);
+            store(a.k_pool + to, a.v_pool + to, c % chunks, held[0], held[32], ks, vs);
+          }
+        }
+        ask(next, stage);
       }
+      first += step;
+      w = next;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  } else {
+    while (first < a.n_rows) {
+      for (int32_t c = lane; c < kRows * chunks; c += 32) {  // (the same trips for every lane: 16 rows of an even number of chunks)
+        const int32_t row = c / chunks, chunk = c - row * chunks;
+        const int64_t from = __shfl_sync(0xffffffffu, w.src, row) + chunk * 16, to = __shfl_sync(0xffffffffu, w.dst, row);
+        const float ks = E8 ? __shfl_sync(0xffffffffu, w.ks, row) : 1.f, vs = E8 ? __shfl_sync(0xffffffffu, w.vs, row) : 1.f;
+        if (to >= 0)
+          store(a.k_pool + to, a.v_pool + to, chunk, *reinterpret_cast<const uint4*>(a.k + from), *reinterpret_cast<const uint4*>(a.v + from), ks, vs);
+      }
+      w = look_on();
+      first += step;
     }
   }
 }
 
 template <typename Kernel, typename Args>
-static purekv_status launch_pdl(Kernel kernel, unsigned blocks, unsigned threads, size_t smem, cudaStream_t stream, const Args& a) {
+static purekv_status launch_pdl(Kernel kernel, dim3 blocks, unsigned threads, size_t smem, cudaStream_t stream, const Args& a) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(blocks);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -285,9 +387,33 @@ static purekv_status launch_pdl(Kernel kernel, unsigned blocks, unsigned threads
 
 template <typename T, bool E8>
 static purekv_status launch_append(const AppendArgs& a, cudaStream_t stream) {
+  const int32_t pairs = a.rows_per_token * (int32_t)a.row_lanes.d, parts = (pairs + kAppendThreads - 1) / kAppendThreads;
+  const unsigned threads = (unsigned)(((pairs + parts - 1) / parts + 31) / 32 * 32);
   const size_t turn = (size_t)a.half * sizeof(float2);
-  if (a.n_tokens <= 148 * 8) return launch_pdl(append_kernel<T, E8, 1>, (unsigned)a.n_tokens, kAppendThreads, turn, stream, a);
-  return launch_pdl(append_kernel<T, E8, 4>, (unsigned)((a.n_tokens + 3) / 4), kAppendThreads, 4 * turn, stream, a);
+  // a token per block while that is not more than the SMs take at once
+  if (a.n_tokens <= 148 * 4) return launch_pdl(append_kernel<T, E8, 1>, dim3((unsigned)a.n_tokens, (unsigned)parts), threads, turn, stream, a);
+  return launch_pdl(append_kernel<T, E8, 4>, dim3((unsigned)((a.n_tokens + 3) / 4), (unsigned)parts), threads, 4 * turn, stream, a);
+}
+
+template <typename T, bool E8, int CH>
+static purekv_status launch_compact_as(const CompactArgs& a, cudaStream_t stream) {
+  constexpr int64_t kRows = 8 * compact_rows<CH>();  // of a block's warps, a batch each
+  auto kernel = compact_paged_kernel<T, E8, CH>;
+  static std::atomic<uint64_t> smem_allowed{0};
+  const purekv_status st = allow_max_dynamic_smem(kernel, smem_allowed);
+  if (st != PUREKV_OK) return st;
+  // as many blocks as the SMs hold at once
+  return launch_pdl(kernel, dim3((unsigned)std::min<int64_t>((a.n_rows + kRows - 1) / kRows, 148 * kCompactBlocks)), 256,
+                    CH ? 8 * kCompactStages * 2048 : 0, stream, a);
+}
+template <typename T, bool E8>
+static purekv_status launch_compact_paged(const CompactArgs& a, cudaStream_t stream) {
+  switch (a.chunks) {
+    case 8: return launch_compact_as<T, E8, 8>(a, stream);
+    case 16: return launch_compact_as<T, E8, 16>(a, stream);
+    case 32: return launch_compact_as<T, E8, 32>(a, stream);
+    default: return launch_compact_as<T, E8, 0>(a, stream);
+  }
 }
 
 }  // namespace purekv
@@ -376,7 +502,6 @@ purekv_status purekv_append_paged(const void* q, int64_t q_token_stride, int64_t
   a.head_dim = head_dim;
   a.rows_per_token = (q ? n_q_heads : 0) + (k ? n_kv_heads : 0) + (v ? n_kv_heads : 0);
   a.row_lanes = FastDiv::of((int32_t)(head_dim * esz / 32));
-  a.rows_div = FastDiv::of(a.rows_per_token);
   cudaStream_t sm = (cudaStream_t)stream;
   if (dtype == PUREKV_FP32) return launch_append<float, false>(a, sm);
   return pages && pages->dtype == PUREKV_E4M3 ? launch_append<__nv_bfloat16, true>(a, sm) : launch_append<__nv_bfloat16, false>(a, sm);
@@ -427,12 +552,10 @@ purekv_status purekv_compact_paged(const void* k, const void* v, int64_t layer_s
     const purekv_status s2 = default_status_word(&a.status);
     if (s2 != PUREKV_OK) return s2;
   }
-  const int64_t blocks = (a.n_rows + 8 * kCompactRows - 1) / (8 * kCompactRows);
-  const unsigned grid = (unsigned)std::min<int64_t>(blocks, 148 * 8);
   cudaStream_t sm = (cudaStream_t)stream;
-  if (dtype == PUREKV_FP32) return launch_pdl(compact_paged_kernel<float, false>, grid, 256, 0, sm, a);
-  return pages->dtype == PUREKV_E4M3 ? launch_pdl(compact_paged_kernel<__nv_bfloat16, true>, grid, 256, 0, sm, a)
-                                     : launch_pdl(compact_paged_kernel<__nv_bfloat16, false>, grid, 256, 0, sm, a);
+  if (dtype == PUREKV_FP32) return launch_compact_paged<float, false>(a, sm);
+  return pages->dtype == PUREKV_E4M3 ? launch_compact_paged<__nv_bfloat16, true>(a, sm)
+                                     : launch_compact_paged<__nv_bfloat16, false>(a, sm);
 }
 
 }  // extern "C"
