@@ -156,11 +156,17 @@ struct RowsAt {
   }
 };
 
+// The rows of a trip that exist, a bit each.
+template <int TK>
+struct MaskOf { using type = uint32_t; };
+template <>
+struct MaskOf<64> { using type = uint64_t; };
+
 // bf16 pools.  Padding of 16 bytes, so that ldmatrix reads eight rows without bank conflicts.
-template <int D_, int NT, bool SW_>
+template <int D_, int NT, int MT, bool SW_>
 struct Bf16Rows {
   static constexpr bool SW = SW_;
-  static constexpr int D = D_, TK = 16, RowBytes = D * 2, KS = RowBytes + (SW ? 0 : 16), VS = KS, R = 8 * NT;
+  static constexpr int D = D_, TK = 16 * MT, RowBytes = D * 2, KS = RowBytes + (SW ? 0 : 16), VS = KS, R = 8 * NT;
   using At = RowsAt<TK, RowBytes, KS, SW>;
   using Out = __nv_bfloat16;
   struct Shared {};
@@ -189,34 +195,43 @@ struct Bf16Rows {
   }
   __device__ __forceinline__ void ready(Shared&) {}
 
-  __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared&, int) {
+  using Mask = typename MaskOf<TK>::type;
+  __device__ __forceinline__ void trip(uint32_t st, Mask mask, Shared&, int) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2;
-    float sc[1][NT][4] = {}, odd[NT][4] = {};  // two chains of products
+    float sc[MT][NT][4] = {}, odd[MT][NT][4] = {};  // two chains of products
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      uint32_t k[4];
-      dec_ldsm(At::at(st, (lane & 7) + 8 * ((lane >> 3) & 1), 2 * ks + (lane >> 4)), k);
+    for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) dec_mma(ks & 1 ? odd[nt] : sc[0][nt], k, qb[ks][nt][0], qb[ks][nt][1]);
-    }
+      for (int mt = 0; mt < MT; ++mt) {
+        uint32_t k[4];
+        dec_ldsm(At::at(st, 16 * mt + (lane & 7) + 8 * ((lane >> 3) & 1), 2 * ks + (lane >> 4)), k);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) dec_mma(ks & 1 ? odd[mt][nt] : sc[mt][nt], k, qb[ks][nt][0], qb[ks][nt][1]);
+      }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sc[0][nt][x] = mask >> (g8 + 8 * (x >> 1)) & 1 ? (sc[0][nt][x] + odd[nt][x]) * unit : -INFINITY;
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? (sc[mt][nt][x] + odd[mt][nt][x]) * unit : -INFINITY;
     float alpha[NT][2];
-    if (dp_softmax<1, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
-    uint32_t p[NT][2];
+    if (dp_softmax<MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      p[nt][0] = dp_transpose(dec_pack_bf16(sc[0][nt][0], sc[0][nt][1]));
-      p[nt][1] = dp_transpose(dec_pack_bf16(sc[0][nt][2], sc[0][nt][3]));
-    }
+    for (int mt = 0; mt < MT; ++mt) {
+      uint32_t p[NT][2];
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) {
-      uint32_t v[4];
-      dec_ldsm_t(At::at(st + TK * KS, (lane & 7) + 8 * (lane >> 4), 2 * n + ((lane >> 3) & 1)), v);
+      for (int nt = 0; nt < NT; ++nt) {
+        p[nt][0] = dp_transpose(dec_pack_bf16(sc[mt][nt][0], sc[mt][nt][1]));
+        p[nt][1] = dp_transpose(dec_pack_bf16(sc[mt][nt][2], sc[mt][nt][3]));
+      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) dec_mma(o[n][nt], v, p[nt][0], p[nt][1]);
+      for (int n = 0; n < D / 16; ++n) {
+        uint32_t v[4];
+        dec_ldsm_t(At::at(st + TK * KS, 16 * mt + (lane & 7) + 8 * (lane >> 4), 2 * n + ((lane >> 3) & 1)), v);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) dec_mma(o[n][nt], v, p[nt][0], p[nt][1]);
+      }
     }
   }
 
@@ -237,11 +252,11 @@ struct Bf16Rows {
 // logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
 // terms is free, so the queries' fragments are laid out to match.  Of the values, ldmatrix transposes pairs of bytes: a register
 // holds two columns of two keys, which go to two tiles, of the even columns and of the odd ones.
-template <int D_, int NT, bool SW_>
+template <int D_, int NT, int MT, bool SW_>
 struct E4m3Rows {
   static constexpr bool SW = SW_;
   // Row strides without bank conflicts: for keys eight lanes read 16 bytes of two rows, for values of eight rows.
-  static constexpr int D = D_, TK = 32, RowBytes = D, KS = SW ? D : D == 128 ? 144 : 64, VS = SW ? D : D + 16, R = 8 * NT, CL = D / 64;
+  static constexpr int D = D_, TK = 16 * MT, RowBytes = D, KS = SW ? D : D == 128 ? 144 : 64, VS = SW ? D : D + 16, R = 8 * NT, CL = D / 64;
   using KAt = RowsAt<TK, RowBytes, KS, SW>;
   using VAt = RowsAt<TK, RowBytes, VS, SW>;
   using Out = __nv_bfloat16;
@@ -308,13 +323,14 @@ struct E4m3Rows {
   }
   __device__ __forceinline__ void ready(Shared&) {}
 
-  __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared&, int) {
+  using Mask = typename MaskOf<TK>::type;
+  __device__ __forceinline__ void trip(uint32_t st, Mask mask, Shared&, int) {
     const int lane = threadIdx.x & 31, g8 = lane >> 2, t = lane & 3;
-    float sc[2][NT][4] = {};
+    float sc[MT][NT][4] = {};
 #pragma unroll
     for (int j = 0; j < CL; ++j)
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
+      for (int mt = 0; mt < MT; ++mt) {
         uint32_t w[2][4];  // keys g8 and g8 + 8
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -330,15 +346,15 @@ struct E4m3Rows {
         }
       }
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
     float alpha[NT][2];
-    if (dp_softmax<2, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
+    if (dp_softmax<MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+    for (int mt = 0; mt < MT; ++mt) {
       uint32_t p[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -420,7 +436,8 @@ struct Fp32Rows {
     }
   }
 
-  __device__ __forceinline__ void trip(uint32_t st, uint32_t mask, Shared& s, int warp) {
+  using Mask = uint32_t;
+  __device__ __forceinline__ void trip(uint32_t st, Mask mask, Shared& s, int warp) {
     const int lane = threadIdx.x & 31, key = lane % TK, part = lane / TK;
     float dot[GP];
 #pragma unroll
@@ -503,8 +520,7 @@ __host__ __device__ constexpr int dp_warp_bytes() {
   return ST * dp_stage_bytes<E>() > E::R * dp_ld<E>() * 4 ? ST * dp_stage_bytes<E>() : E::R * dp_ld<E>() * 4;
 }
 // Partial results of one slot: [R][D] unnormalised outputs, [R] references, [R] sums
-template <class E>
-__host__ __device__ constexpr int64_t dp_part_floats() { return (int64_t)E::R * (E::D + 2); }
+__host__ __device__ constexpr int64_t dp_part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
 
 // What a run of the balanced form leaves: the request and virtual head whose first part it is (in its second slot), and how many
 // parts there are (the others in the first slots of the head's runs that follow); 0: nothing.
@@ -529,9 +545,11 @@ __device__ __forceinline__ void dp_store4(float* dst, float4 v) { *reinterpret_c
 // How rows come into shared memory: each by its own page (cp.async); a trip's rows from one page (cp.async), where a page holds whole
 // trips; the same by the copy engine.
 enum DpLoad { kDpRows, kDpWhole, kDpEngine };
-// The pools as the copy engine sees them, in bytes: (128 of a row, slot of a page, part of a row, head, page).
+// The pools as the copy engine sees them, in bytes: (128 of a row, slot of a page, part of a row, head, page).  A trip's rows are `boxes`
+// boxes: one of all parts where a page holds whole trips, otherwise one for each part and page.
 struct DpMaps {
   CUtensorMap k, v;
+  int32_t boxes;
 };
 
 template <class E, int W, int ST, bool CLUSTER, DpLoad LOAD, int OCC>
@@ -545,7 +563,8 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   // (the swizzle counts from multiples of 1024 bytes)
   uint8_t* const dp_smem = LOAD == kDpEngine ? dp_smem_raw + (-(int32_t)__cvta_generic_to_shared(dp_smem_raw) & 1023) : dp_smem_raw;
   __shared__ float s_ml[W][R][2];
-  __shared__ uint32_t s_mask[W][ST];
+  using Mask = typename E::Mask;
+  __shared__ Mask s_mask[W][ST];
   __shared__ __align__(8) uint64_t s_full[LOAD == kDpEngine ? W : 1][ST];  // a stage's copies have arrived
   __shared__ int s_late;
   __shared__ __align__(16) typename E::Shared s_e;
@@ -707,13 +726,16 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     }
   };
 
+  const int32_t box_rows = LOAD == kDpEngine ? TK / maps.boxes : TK;
+
   // ---- loads.  The cursor runs ahead of the products, over the ends of requests and of runs.
   DpRun f = run;
   int32_t f_answers = 0, f_runs = 1;  // answers read, runs entered
   bool f_more = !CLUSTER, f_empty = false;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dp_smem) + (uint32_t)warp * kWarpBytes;
-  // The page of a row, its slot there and its KV head.  WHOLE (a page holds whole trips): of the trip's first row, `there` of whose
-  // rows are wanted; otherwise of row `lane` of the trip, `there` 1 if it is wanted.
+  // The page of a row, its slot there and its KV head.  WHOLE: of the trip's first row, `there` of whose rows are wanted (copy engine:
+  // of the first row of box `lane`, if there are several, and of that box); otherwise of row `lane` of the trip, `there` 1 if it is
+  // wanted.
   struct Look {
     int32_t page, slot, g, there;
   };
@@ -739,8 +761,13 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
     }
     if (f.left > 0) {
-      const int32_t row = f.tile * TILE + warp * TK + (WHOLE ? 0 : lane);
-      k.there = WHOLE ? min(max(f.n - row, 0), TK) : lane < TK && row < f.n;
+      int32_t row = f.tile * TILE + warp * TK + (WHOLE ? 0 : lane);
+      if constexpr (LOAD == kDpEngine) {
+        if (maps.boxes > 1) row += lane * box_rows;
+        k.there = maps.boxes == 1 || lane < maps.boxes ? min(max(f.n - row, 0), box_rows) : 0;
+      } else {
+        k.there = WHOLE ? min(max(f.n - row, 0), TK) : lane < TK && row < f.n;
+      }
       if (k.there > 0) {
         const uint32_t p = a.view.page_size.quotient((uint32_t)row);
         k.slot = row - (int32_t)(p * a.view.page_size.d);
@@ -764,22 +791,43 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const uint32_t dst = ring + (uint32_t)stage * kStage + (lane / CPR) * E::KS + (lane % CPR) * 16;
     const uint32_t dst_v = ring + (uint32_t)stage * kStage + TK * E::KS + (lane / CPR) * E::VS + (lane % CPR) * 16;
     const int64_t off = k.there > 0 ? a.view.offset(k.page, (uint32_t)k.slot) : -1;
-    uint32_t mask;
+    Mask mask;
     if constexpr (LOAD == kDpEngine) {
-      mask = off < 0 ? 0u : k.there == 32 ? 0xffffffffu : (1u << k.there) - 1u;
+      mask = off < 0 ? (Mask)0 : (Mask)(~(Mask)0 >> (8 * sizeof(Mask) - k.there));
+      uint32_t rows = off >= 0 ? (uint32_t)box_rows : 0u;  // copied: whole boxes; what lies behind the request's last row is masked (keys) or overwritten (values) later
+      bool missing = k.there > 0 && off < 0;
+      if (maps.boxes > 1) {
+        mask = off < 0 ? (Mask)0 : mask << (lane * box_rows);
+        uint32_t lo = __reduce_or_sync(0xffffffffu, (uint32_t)mask);
+        if constexpr (sizeof(Mask) == 8) mask = lo | (Mask)__reduce_or_sync(0xffffffffu, (uint32_t)(mask >> 32)) << 32;
+        else mask = lo;
+        rows = __popc(__ballot_sync(0xffffffffu, off >= 0)) * box_rows;
+        missing = __any_sync(0xffffffffu, missing);
+      }
+      const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), to = ring + (uint32_t)stage * kStage;
+      auto load = [&](uint32_t dst, const CUtensorMap* map, int32_t part, int32_t slot, int32_t page) {
+        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                     ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(slot), "r"(part), "r"(k.g), "r"(page) : "memory");
+      };
       if (lane == 0) {
-        if (k.there > 0 && off < 0) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
-        const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), to = ring + (uint32_t)stage * kStage;
-        if (mask) {  // whole trips: what lies behind the request's last row is masked (keys) or overwritten (values) later
-          tc::mbar_expect_tx(bar, 2 * TK * E::RowBytes);
-          auto load = [&](uint32_t dst, const CUtensorMap* map) {
-            asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-                         ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(k.slot), "r"(0), "r"(k.g), "r"(k.page) : "memory");
-          };
-          load(to, &maps.k);
-          load(to + TK * E::KS, &maps.v);
-        } else {
-          tc::mbar_arrive(bar);  // (the barrier's phases stay in step with the stages)
+        if (missing) atomicExch(a.status, (int32_t)PUREKV_ERR_BAD_PAGE);
+        if (rows) tc::mbar_expect_tx(bar, rows * 2 * E::RowBytes);
+        else tc::mbar_arrive(bar);  // (the barrier's phases stay in step with the stages)
+      }
+      if (maps.boxes == 1) {
+        if (lane == 0 && rows) {
+          load(to, &maps.k, 0, k.slot, k.page);
+          load(to + TK * E::KS, &maps.v, 0, k.slot, k.page);
+        }
+      } else {
+        constexpr int kParts = E::RowBytes < 128 ? 1 : E::RowBytes / 128, kInner = E::RowBytes / kParts;
+        __syncwarp();  // (the barrier expects the bytes before they come)
+        const int32_t box = lane % maps.boxes, part = lane / maps.boxes;
+        const int32_t page = __shfl_sync(0xffffffffu, off >= 0 ? k.page : -1, box);
+        if (page >= 0 && part < kParts) {
+          const uint32_t dst = to + part * (TK * kInner) + box * box_rows * kInner;
+          load(dst, &maps.k, part, 0, page);
+          load(dst + TK * E::KS, &maps.v, part, 0, page);
         }
       }
     } else if constexpr (WHOLE) {
@@ -857,14 +905,14 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
       const bool ok = arrived(stage, phase);
       __syncwarp();
-      const uint32_t mask = ok ? s_mask[warp][stage] : 0u;
+      const Mask mask = ok ? s_mask[warp][stage] : (Mask)0;
       if constexpr (LOAD == kDpEngine) {
-        constexpr uint32_t kAll = TK == 32 ? 0xffffffffu : (1u << TK) - 1u;
-        if (mask != 0u && mask != kAll) {  // zeros for the values that are not the request's: whatever lies there has weight 0, but may be NaN
+        constexpr Mask kAll = (Mask)(~(Mask)0 >> (8 * sizeof(Mask) - TK));
+        if (mask != 0 && mask != kAll) {  // zeros for the values that are not the request's: whatever lies there has weight 0, but may be NaN
           constexpr int kChunks = E::RowBytes / 16, kPart = kChunks < 8 ? kChunks : 8;  // of a row, of a part of a row
-          const int32_t there = __popc(mask);
-          for (int32_t x = lane; x < (TK - there) * kChunks; x += 32) {
-            const int32_t row = there + x / kChunks, c = x % kChunks;
+          for (int32_t x = lane; x < TK * kChunks; x += 32) {
+            const int32_t row = x / kChunks, c = x % kChunks;
+            if (mask >> row & 1) continue;
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (uint32_t)stage * kStage + TK * E::KS + (c / kPart) * (TK * 128) + row * (kPart * 16) + (c % kPart) * 16), "r"(0) : "memory");
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the copy engine writes there again
@@ -918,7 +966,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     const bool whole = CLUSTER ? C == 1 : from_start && end_of_request;
     const int32_t cols = D / C;  // columns of every head that each CTA of the cluster finishes
     float* slot = nullptr;
-    if constexpr (!CLUSTER) slot = a.part + (2 * (int64_t)done.id + (from_start ? 1 : 0)) * dp_part_floats<E>();
+    if constexpr (!CLUSTER) slot = a.part + (2 * (int64_t)done.id + (from_start ? 1 : 0)) * dp_part_floats(R, D);
     for (int32_t x = tid; x < nh_done * (D / 4); x += kThreads) {  // one thread per four columns of a head
       const int32_t h = x / (D / 4), col = 4 * (x % (D / 4));
       float top = -INFINITY;
@@ -1021,11 +1069,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 // sixteen parts at a time, all loads of which are asked for before the first is used, and runs a softmax of its own over them; the groups meet in
 // shared memory.  Many chains of few parts: a block each, all heads (J 1, HPB 8).  Few chains, of many parts: a head each (J 8, HPB 1).
 // Requests without rows get their zeros here.
-template <class E, int HPB, int J>
+template <typename Out, int D, int R, int HPB, int J>
 __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
-  constexpr int D = E::D, R = E::R, kHead = D / 4, kGroup = HPB * kHead, kGroups = 256 / kGroup, kAtOnce = J == 1 ? 16 : 8;
+  constexpr int kHead = D / 4, kGroup = HPB * kHead, kGroups = 256 / kGroup, kAtOnce = J == 1 ? 16 : 8;
   static_assert(kGroups >= 1, "a head's columns fit a block");
-  using Out = typename E::Out;
   __shared__ float s_ml[kGroups][HPB][2];
   __shared__ __align__(16) float4 s_acc[kGroups][kGroup];
   const int32_t grp = threadIdx.x / kGroup, in_grp = threadIdx.x % kGroup, hb = in_grp / kHead, c = in_grp % kHead, h = blockIdx.y * HPB + hb;
@@ -1066,7 +1113,7 @@ __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_con
         li[k] = 0.f;
         v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i < chain.parts) {
-          const float* slot = a.part + (2 * (first + (int64_t)i * a.v_heads) + (i == 0 ? 1 : 0)) * dp_part_floats<E>();
+          const float* slot = a.part + (2 * (first + (int64_t)i * a.v_heads) + (i == 0 ? 1 : 0)) * dp_part_floats(R, D);
           mi[k] = slot[R * D + h];
           li[k] = slot[R * D + R + h];
           v[k] = *reinterpret_cast<const float4*>(slot + h * D + 4 * c);
@@ -1178,9 +1225,9 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
   const int32_t heads = std::min(E::R, a.group);
   DpLaunch j(many ? dim3((unsigned)runs, (unsigned)((heads + kWide - 1) / kWide)) : dim3((unsigned)((runs + 7) / 8), (unsigned)heads), 256, 0, stream);
   if (many)
-    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E, kWide, 1>, a));
+    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<typename E::Out, E::D, E::R, kWide, 1>, a));
   else
-    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<E, 1, 8>, a));
+    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<typename E::Out, E::D, E::R, 1, 8>, a));
   return PUREKV_OK;
 }
 
@@ -1202,12 +1249,15 @@ static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t bound) {
 template <class E>
 static bool dp_maps(const DecodePagedArgs& a, int32_t n_kv_heads, DpMaps* maps) {
   const tc::EncodeTiledFn encode = tc::encode_fn();
-  if (!encode) return false;
+  if (!encode || a.view.n_pages == 0) return false;
   constexpr cuuint32_t kInner = E::RowBytes < 128 ? E::RowBytes : 128, kParts = E::RowBytes / kInner;
   auto stride = [](int64_t s) { return (cuuint64_t)(s > 0 ? s : E::RowBytes); };  // (0: a dimension of size 1)
   const cuuint64_t dims[5] = {kInner, (cuuint64_t)a.view.page_size.d, kParts, (cuuint64_t)n_kv_heads, (cuuint64_t)a.view.n_pages};
   const cuuint64_t strides[4] = {stride(a.view.token_stride), 128, stride(a.view.head_stride), stride(a.view.page_stride)};
-  const cuuint32_t box[5] = {kInner, (cuuint32_t)E::TK, kParts, 1, 1}, each[5] = {1, 1, 1, 1, 1};
+  const bool whole = a.view.page_size.d % E::TK == 0;
+  if (!whole && (E::TK % a.view.page_size.d || a.view.page_size.d < 8)) return false;  // (the swizzle repeats every eight rows)
+  maps->boxes = whole ? 1 : E::TK / (int32_t)a.view.page_size.d;
+  const cuuint32_t box[5] = {kInner, (cuuint32_t)(E::TK / maps->boxes), whole ? kParts : 1, 1, 1}, each[5] = {1, 1, 1, 1, 1};
   const uint8_t* pools[2] = {a.k_pool, a.v_pool};
   CUtensorMap* out[2] = {&maps->k, &maps->v};
   for (int i = 0; i < 2; ++i)
@@ -1223,10 +1273,10 @@ static bool dp_maps(const DecodePagedArgs& a, int32_t n_kv_heads, DpMaps* maps) 
 // eight warps in a CTA and with two CTAs of four.
 template <class E, class X, int ST8, int ST4>
 static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
-  const bool whole = a.view.page_size.d % E::TK == 0 && a.view.n_pages > 0;
+  const bool whole = a.view.page_size.d % E::TK == 0;
   if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
   DpMaps maps = {};
-  if (whole && dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, 2>(a, maps, stream);
+  if (dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, 2>(a, maps, stream);
   return launch_balanced<E, 4, ST8, kDpRows, 2>(a, maps, stream);
 }
 
@@ -1308,17 +1358,20 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   }
   cudaStream_t sm = (cudaStream_t)stream;
   const bool wide = pages->head_dim == 128;
-#define PK_ROWS(ENGINE, D, N, ST8, ST4) launch_rows<ENGINE<D, N, false>, ENGINE<D, N, true>, ST8, ST4>(a, pages->n_kv_heads, form, sm)
+  // rows of a trip: 8 KB of K and V, or 4 where threads look a row up each
+#define PK_FP32(D, N) launch_rows<Fp32Rows<D, N, false>, Fp32Rows<D, N, true>, 3, 3>(a, pages->n_kv_heads, form, sm)
+#define PK_ROWS(ENGINE, D, N, MT, MT4, ST8, ST4) launch_rows<ENGINE<D, N, MT, false>, ENGINE<D, N, MT4, true>, ST8, ST4>(a, pages->n_kv_heads, form, sm)
   if (dtype == PUREKV_FP32) {
-    if (rows == 2) return wide ? PK_ROWS(Fp32Rows, 128, 2, 3, 3) : PK_ROWS(Fp32Rows, 64, 2, 3, 3);
-    return wide ? PK_ROWS(Fp32Rows, 128, 8, 3, 3) : PK_ROWS(Fp32Rows, 64, 8, 3, 3);
+    if (rows == 2) return wide ? PK_FP32(128, 2) : PK_FP32(64, 2);
+    return wide ? PK_FP32(128, 8) : PK_FP32(64, 8);
   }
   if (pages->dtype == PUREKV_E4M3) {
-    if (rows == 8) return wide ? PK_ROWS(E4m3Rows, 128, 1, 3, 3) : PK_ROWS(E4m3Rows, 64, 1, 5, 6);
-    return wide ? PK_ROWS(E4m3Rows, 128, 2, 2, 3) : PK_ROWS(E4m3Rows, 64, 2, 5, 6);
+    if (rows == 8) return wide ? PK_ROWS(E4m3Rows, 128, 1, 2, 2, 3, 3) : PK_ROWS(E4m3Rows, 64, 1, 2, 4, 5, 3);
+    return wide ? PK_ROWS(E4m3Rows, 128, 2, 2, 2, 2, 3) : PK_ROWS(E4m3Rows, 64, 2, 2, 4, 5, 3);
   }
-  if (rows == 8) return wide ? PK_ROWS(Bf16Rows, 128, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 1, 5, 6);
-  return wide ? PK_ROWS(Bf16Rows, 128, 2, 3, 3) : PK_ROWS(Bf16Rows, 64, 2, 5, 6);
+  if (rows == 8) return wide ? PK_ROWS(Bf16Rows, 128, 1, 1, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 1, 1, 2, 5, 3);
+  return wide ? PK_ROWS(Bf16Rows, 128, 2, 1, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 2, 1, 2, 5, 3);
+#undef PK_FP32
 #undef PK_ROWS
 }
 
