@@ -1235,14 +1235,30 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
 // head.
 struct DpForm {
   int32_t cluster, at_once, n_long, n_short;
+  int32_t per_sm = 1;  // even form: CTAs per SM, of eight warps (1) or four (2, and 3 with a ring of one stage)
 };
-static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t bound) {
-  const int64_t base = n_req * v_heads;
+// Measured over 1-128 requests of 16-64 000 rows, 4 and 2 KV heads, all three types (us).  A CTA alone on its SM streams 75 GB/s, all
+// together 6.3 TB/s; the even form costs 4 us besides, the balanced one 14.  Clusters: as many CTAs as find an SM each (128, or 64 for
+// clusters of eight and more: 4 requests of 1000 bf16 rows 7.8 with 4 CTAs each, 10.4 with 8), but not for less than 150 KB of
+// a head's rows (200 bf16 rows: 4.7 with one CTA, 5.4 with 16; 500: 7.3 and 5.4), and no pairs for less than 512 KB (64 heads of 500
+// rows: 7.8 alone, 9.3 in pairs).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all requests are as
+// long as the longest, but nothing says so (128 of 2900-5100 rows: 170 against 180; one of 60 000 among 63 of 100-2000: 57 against 450), and
+// where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
+static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int64_t row_bytes) {
+  const int64_t base = n_req * v_heads, bytes = longest * row_bytes;  // of one head's rows
   int32_t c = 1;
-  while (c < kDpClusterMax && bound > 128 * c && base * 2 * c <= (c < 4 ? 128 : 64)) c *= 2;
-  if (bound <= 128 * (int64_t)c * 2) return {c, 0, 0, 0};
-  const int32_t at_once = kDpAtOnce, shorts = kDpShorts * at_once;
-  return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((shorts + v_heads - 1) / v_heads)};
+  if (bytes > 150000) {
+    while (c < kDpClusterMax && longest > 64 * c && base * 2 * c <= (c < 4 ? 128 : 64)) c *= 2;
+    if (c == 2 && bytes <= 512000) c = 1;
+  }
+  const double all = (double)base * bytes / 6.3e6, share = (double)((base * c + 147) / 148) * bytes / c / 75e3;
+  if (all < 60. && std::max(all, share) + 4. < all + 14.) {
+    // more heads than SMs: several CTAs of four warps on each, so that one streams while another starts or ends
+    const int32_t per_sm = base <= 148 || longest > 2048 ? 1 : longest > 64 ? 2 : 3;
+    return {c, 0, 0, 0, per_sm};
+  }
+  constexpr int64_t kShorts = kDpShorts * kDpAtOnce;
+  return {0, kDpAtOnce, (int32_t)std::max<int64_t>(1, kDpAtOnce / v_heads), (int32_t)((kShorts + v_heads - 1) / v_heads)};
 }
 
 // The pools for the copy engine; false where it cannot take them.
@@ -1274,6 +1290,8 @@ static bool dp_maps(const DecodePagedArgs& a, int32_t n_kv_heads, DpMaps* maps) 
 template <class E, class X, int ST8, int ST4>
 static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
   const bool whole = a.view.page_size.d % E::TK == 0;
+  if (f.cluster && f.per_sm == 3) return launch_even<E, 4, 1, kDpRows, (E::R > 8 ? 2 : 3)>(a, f.cluster, stream);
+  if (f.cluster && f.per_sm == 2) return launch_even<E, 4, 3, kDpRows, 2>(a, f.cluster, stream);
   if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
   DpMaps maps = {};
   if (dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, 2>(a, maps, stream);
@@ -1299,7 +1317,10 @@ size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_
   if (n_req <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || head_dim <= 0) return 0;
   const int32_t group = n_q_heads / n_kv_heads, rows = dp_rows(group, dtype), blocks = (group + rows - 1) / rows;
   const int64_t v_heads = (int64_t)n_kv_heads * blocks;
-  return (size_t)dp_ws(dp_form(n_req, v_heads, max_len > 0 ? max_len : INT32_MAX), v_heads, group, head_dim, dtype);
+  // (of the pools' types that go with dtype, e4m3 has the shorter rows: either may need the larger workspace)
+  const int64_t longest = max_len > 0 ? max_len : INT32_MAX, row = 2 * head_dim * (dtype == PUREKV_FP32 ? 4 : 2);
+  return (size_t)std::max(dp_ws(dp_form(n_req, v_heads, longest, row), v_heads, group, head_dim, dtype),
+                          dtype == PUREKV_FP32 ? 0 : dp_ws(dp_form(n_req, v_heads, longest, row / 2), v_heads, group, head_dim, dtype));
 }
 
 purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t q_head_stride, void* o, float* lse,
@@ -1341,7 +1362,7 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   a.o = o;
   a.lse = lse;
   a.status = status;
-  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX);
+  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX, 2 * pages->head_dim * bytes_of(pages->dtype));
   if (!form.cluster) {
     PK_REQUIRE(ws && ws_bytes >= (size_t)dp_ws(form, a.v_heads, a.group, pages->head_dim, dtype), PUREKV_ERR_WORKSPACE,
                "%s: workspace of %zu bytes is too small", kName, ws_bytes);
