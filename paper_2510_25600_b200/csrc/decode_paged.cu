@@ -55,7 +55,7 @@ constexpr int kDpGroups = 128;   // of requests: their running sums of tiles lie
 constexpr int kDpSteals = 8;     // answers to requests for runs that a CTA keeps: more than runs its loads can be ahead of its products
 // Three quarters of a CTA's share of the tiles make its long run; the rest is cut into short runs, three for every CTA at work, of four
 // tiles at least, which go to whichever CTA asks next.
-constexpr int kDpAtOnce = 296, kDpShorts = 3, kDpShortest = 4;  // CTAs at work: two per SM
+constexpr int kDpShorts = 3, kDpShortest = 4;
 
 // Tiles of one head: `left` of them, from tile `tile` of request r (n rows) on, tile `at` of the head's.
 struct DpRun {
@@ -1244,7 +1244,7 @@ struct DpForm {
 // rows: 7.8 alone, 9.3 in pairs).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all requests are as
 // long as the longest, but nothing says so (128 of 2900-5100 rows: 170 against 180; one of 60 000 among 63 of 100-2000: 57 against 450), and
 // where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
-static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int64_t row_bytes) {
+static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int64_t row_bytes, int32_t at_once) {
   const int64_t base = n_req * v_heads, bytes = longest * row_bytes;  // of one head's rows
   int32_t c = 1;
   if (bytes > 150000) {
@@ -1257,8 +1257,7 @@ static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int64_t r
     const int32_t per_sm = base <= 148 || longest > 2048 ? 1 : longest > 64 ? 2 : 3;
     return {c, 0, 0, 0, per_sm};
   }
-  constexpr int64_t kShorts = kDpShorts * kDpAtOnce;
-  return {0, kDpAtOnce, (int32_t)std::max<int64_t>(1, kDpAtOnce / v_heads), (int32_t)((kShorts + v_heads - 1) / v_heads)};
+  return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((kDpShorts * at_once + v_heads - 1) / v_heads)};
 }
 
 // The pools for the copy engine; false where it cannot take them.
@@ -1287,18 +1286,24 @@ static bool dp_maps(const DecodePagedArgs& a, int32_t n_kv_heads, DpMaps* maps) 
 
 // E: the engine for rows copied by threads; X: the same for rows that the copy engine brings.  ST8 and ST4: stages of each warp with
 // eight warps in a CTA and with two CTAs of four.
-template <class E, class X, int ST8, int ST4>
+template <class E, class X, int ST8, int ST4, int OCC4>
 static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
   const bool whole = a.view.page_size.d % E::TK == 0;
   if (f.cluster && f.per_sm == 3) return launch_even<E, 4, 1, kDpRows, (E::R > 8 ? 2 : 3)>(a, f.cluster, stream);
   if (f.cluster && f.per_sm == 2) return launch_even<E, 4, 3, kDpRows, 2>(a, f.cluster, stream);
   if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
   DpMaps maps = {};
-  if (dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, 2>(a, maps, stream);
-  return launch_balanced<E, 4, ST8, kDpRows, 2>(a, maps, stream);
+  if (dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, OCC4>(a, maps, stream);
+  return launch_balanced<E, 4, OCC4 == 3 ? 2 : ST8, kDpRows, OCC4>(a, maps, stream);
 }
 
+
 static int32_t dp_rows(int32_t group, purekv_dtype dtype) { return dtype == PUREKV_FP32 ? (group <= 2 ? 2 : 8) : group <= 8 ? 8 : 16; }
+
+// CTAs of the balanced form at work: two per SM, or three where the products and not the loads take the time: of e4m3, which has to
+// become fp16, with up to eight heads (128 requests of 2900-5100 rows, 8 KV heads, pages of 16 rows: 201 us with two, 176 with three; of 64 rows 185 and 183).
+constexpr int dp_ctas(bool e4m3, int rows) { return e4m3 && rows == 8 ? 3 : 2; }
+static int32_t dp_at_once(int32_t rows, purekv_dtype held) { return 148 * dp_ctas(held == PUREKV_E4M3, rows); }
 
 static int64_t dp_ws(const DpForm& f, int64_t v_heads, int32_t group, int32_t head_dim, purekv_dtype dtype) {
   if (f.cluster) return 0;
@@ -1318,9 +1323,12 @@ size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_
   const int32_t group = n_q_heads / n_kv_heads, rows = dp_rows(group, dtype), blocks = (group + rows - 1) / rows;
   const int64_t v_heads = (int64_t)n_kv_heads * blocks;
   // (of the pools' types that go with dtype, e4m3 has the shorter rows: either may need the larger workspace)
-  const int64_t longest = max_len > 0 ? max_len : INT32_MAX, row = 2 * head_dim * (dtype == PUREKV_FP32 ? 4 : 2);
-  return (size_t)std::max(dp_ws(dp_form(n_req, v_heads, longest, row), v_heads, group, head_dim, dtype),
-                          dtype == PUREKV_FP32 ? 0 : dp_ws(dp_form(n_req, v_heads, longest, row / 2), v_heads, group, head_dim, dtype));
+  const int64_t longest = max_len > 0 ? max_len : INT32_MAX;
+  auto need = [&](purekv_dtype held) {
+    const DpForm f = dp_form(n_req, v_heads, longest, 2 * head_dim * bytes_of(held), dp_at_once(rows, held));
+    return dp_ws(f, v_heads, group, head_dim, dtype);
+  };
+  return (size_t)std::max(need(dtype), dtype == PUREKV_FP32 ? 0 : need(PUREKV_E4M3));
 }
 
 purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t q_head_stride, void* o, float* lse,
@@ -1362,7 +1370,8 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   a.o = o;
   a.lse = lse;
   a.status = status;
-  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX, 2 * pages->head_dim * bytes_of(pages->dtype));
+  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX, 2 * pages->head_dim * bytes_of(pages->dtype),
+                              dp_at_once(rows, pages->dtype));
   if (!form.cluster) {
     PK_REQUIRE(ws && ws_bytes >= (size_t)dp_ws(form, a.v_heads, a.group, pages->head_dim, dtype), PUREKV_ERR_WORKSPACE,
                "%s: workspace of %zu bytes is too small", kName, ws_bytes);
@@ -1380,18 +1389,18 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   cudaStream_t sm = (cudaStream_t)stream;
   const bool wide = pages->head_dim == 128;
   // rows of a trip: 8 KB of K and V, or 4 where threads look a row up each
-#define PK_FP32(D, N) launch_rows<Fp32Rows<D, N, false>, Fp32Rows<D, N, true>, 3, 3>(a, pages->n_kv_heads, form, sm)
-#define PK_ROWS(ENGINE, D, N, MT, MT4, ST8, ST4) launch_rows<ENGINE<D, N, MT, false>, ENGINE<D, N, MT4, true>, ST8, ST4>(a, pages->n_kv_heads, form, sm)
+#define PK_FP32(D, N) launch_rows<Fp32Rows<D, N, false>, Fp32Rows<D, N, true>, 3, 3, 2>(a, pages->n_kv_heads, form, sm)
+#define PK_ROWS(ENGINE, D, N, MT, MT4, ST8, ST4, OCC4) launch_rows<ENGINE<D, N, MT, false>, ENGINE<D, N, MT4, true>, ST8, ST4, OCC4>(a, pages->n_kv_heads, form, sm)
   if (dtype == PUREKV_FP32) {
     if (rows == 2) return wide ? PK_FP32(128, 2) : PK_FP32(64, 2);
     return wide ? PK_FP32(128, 8) : PK_FP32(64, 8);
   }
   if (pages->dtype == PUREKV_E4M3) {
-    if (rows == 8) return wide ? PK_ROWS(E4m3Rows, 128, 1, 2, 2, 3, 3) : PK_ROWS(E4m3Rows, 64, 1, 2, 4, 5, 3);
-    return wide ? PK_ROWS(E4m3Rows, 128, 2, 2, 2, 2, 3) : PK_ROWS(E4m3Rows, 64, 2, 2, 4, 5, 3);
+    if (rows == 8) return wide ? PK_ROWS(E4m3Rows, 128, 1, 2, 2, 3, 2, 3) : PK_ROWS(E4m3Rows, 64, 1, 2, 4, 5, 2, 3);
+    return wide ? PK_ROWS(E4m3Rows, 128, 2, 2, 2, 2, 3, 2) : PK_ROWS(E4m3Rows, 64, 2, 2, 4, 5, 3, 2);
   }
-  if (rows == 8) return wide ? PK_ROWS(Bf16Rows, 128, 1, 1, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 1, 1, 2, 5, 3);
-  return wide ? PK_ROWS(Bf16Rows, 128, 2, 1, 1, 3, 3) : PK_ROWS(Bf16Rows, 64, 2, 1, 2, 5, 3);
+  if (rows == 8) return wide ? PK_ROWS(Bf16Rows, 128, 1, 1, 1, 3, 3, 2) : PK_ROWS(Bf16Rows, 64, 1, 1, 2, 5, 3, 2);
+  return wide ? PK_ROWS(Bf16Rows, 128, 2, 1, 1, 3, 3, 2) : PK_ROWS(Bf16Rows, 64, 2, 1, 2, 5, 3, 2);
 #undef PK_FP32
 #undef PK_ROWS
 }
