@@ -400,7 +400,8 @@ purekv_status purekv_compact_paged(const void *k, const void *v, int64_t layer_s
  * A request with seq_lens[r] <= 0 gets o = 0 and lse = -inf.  head_dim 64 or 128; any number of query heads per KV head; dtype (q and o) BF16 with pools
  * of BF16 or E4M3, or FP32 with FP32 pools.  max_len only sizes the launch: the longest request that is to be expected,
  * 0 if unknown; longer requests are served all the same.  ws: purekv_decode_paged_ws_bytes for the same sizes (nullable
- * when that is 0), not initialised; calls that may run at the same time need one each.  softmax_scale <= 0 means 1/sqrt(d). */
+ * when that is 0), not initialised; calls that may run at the same time need one each.  softmax_scale <= 0 means 1/sqrt(d).  Waits
+ * are bounded as in the tensor-core prefill (PUREKV_ERR_TIMEOUT in the status word: o and lse are then undefined). */
 size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                     purekv_dtype dtype);
 purekv_status purekv_decode_paged(const void *q, int64_t q_token_stride, int64_t q_head_stride, void *o, float *lse,

@@ -1098,9 +1098,12 @@ __global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_con
 #pragma unroll
   for (int which = 0; which < J; ++which) {
     const ChainRecord chain = chains[which];
-    const int32_t g = a.blocks == 1 ? chain.vh : chain.vh / a.blocks, b = chain.vh - g * a.blocks, nh = min(R, a.group - b * R);
-    if (chain.parts == 0) continue;  // the same for the block
     const int64_t first = blockIdx.x + (int64_t)which * gridDim.x;
+    // the same for the block.  (A record is always whole, unless a wait ran out or the lengths changed under the kernels: then it may be
+    // anything, and nothing follows it anywhere.)
+    if (chain.parts <= 0 || chain.r < 0 || chain.r >= a.n_req || chain.vh < 0 || chain.vh >= a.v_heads || first + (int64_t)(chain.parts - 1) * a.v_heads >= runs)
+      continue;
+    const int32_t g = a.blocks == 1 ? chain.vh : chain.vh / a.blocks, b = chain.vh - g * a.blocks, nh = min(R, a.group - b * R);
     float ref = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int32_t i0 = grp; i0 < chain.parts && h < nh; i0 += kAtOnce * kGroups) {

@@ -18,7 +18,7 @@ inline purekv_status check_pages(const purekv_pages* p, purekv_dtype dtype, cons
              "%s: bf16 goes with pools of bf16 or e4m3, fp32 with pools of fp32", where);
   PK_REQUIRE(p->dtype == PUREKV_E4M3 || (!p->k_scale && !p->v_scale), PUREKV_ERR_INVALID_ARG, "%s: only e4m3 pools have scales", where);
   if (p->n_req == 0) return PUREKV_OK;
-  PK_REQUIRE(p->block_table && p->seq_lens, PUREKV_ERR_INVALID_ARG, "%s: null block_table or seq_lens", where);
+  PK_REQUIRE((p->block_table || p->max_pages == 0) && p->seq_lens, PUREKV_ERR_INVALID_ARG, "%s: null block_table or seq_lens", where);
   PK_REQUIRE(p->n_req == 1 || p->table_stride >= p->max_pages, PUREKV_ERR_INVALID_ARG, "%s: rows of the block table overlap", where);
   PK_REQUIRE(p->n_pages == 0 || (p->k && p->v), PUREKV_ERR_INVALID_ARG, "%s: null pool", where);
   PK_REQUIRE(((uintptr_t)p->k | (uintptr_t)p->v) % 16 == 0, PUREKV_ERR_INVALID_ARG, "%s: pools must be 16-byte aligned", where);

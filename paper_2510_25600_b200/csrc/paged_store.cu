@@ -518,7 +518,7 @@ purekv_status purekv_compact_paged(const void* k, const void* v, int64_t layer_s
   PK_REQUIRE(n_layers >= 0 && k_tot >= 0 && total_tokens >= 0 && total_tokens <= INT32_MAX, PUREKV_ERR_INVALID_ARG, "%s: bad sizes", kName);
   if (n_layers == 0 || k_tot == 0 || pages->n_req == 0) return PUREKV_OK;
   PK_REQUIRE(k && v && idx && cu_seqlens && cu_kept, PUREKV_ERR_INVALID_ARG, "%s: null pointer", kName);
-  PK_REQUIRE((int64_t)k_tot * pages->n_kv_heads <= INT32_MAX, PUREKV_ERR_UNSUPPORTED, "%s: too many rows in a layer", kName);
+  PK_REQUIRE((int64_t)k_tot * pages->n_kv_heads <= 1 << 30, PUREKV_ERR_UNSUPPORTED, "%s: too many rows in a layer", kName);
   PK_REQUIRE(pages->head_dim % 16 == 0 && pages->head_dim <= 512, PUREKV_ERR_UNSUPPORTED,
              "%s: head_dim must be a multiple of 16, at most 512", kName);
   const int64_t esz = dtype == PUREKV_BF16 ? 2 : 4, out_esz = bytes_of(pages->dtype);

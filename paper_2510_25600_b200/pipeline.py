@@ -152,8 +152,9 @@ class PureKVPipeline:
                 events[layer][1].record()
         self.prefill_launches += hi - lo
 
-    def run_device(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, events=None, marks=None) -> None:
-        """q [n_layers,T,H,d], k,v [kv_layers,T,H_kv,d] on the GPU.  Results in self.o / idx / k_c / v_c.
+    def run_device(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, events=None, marks=None, pages=None) -> None:
+        """q [n_layers,T,H,d], k,v [kv_layers,T,H_kv,d] on the GPU.  Results in self.o / idx / k_c / v_c; with `pages`, a PagedCache of
+        as many layers as are compacted, the kept rows go there instead of k_c / v_c, behind what its conversations have.
         `events`, if given, is a list of (start, end) torch.cuda.Event pairs, one per layer, which is then a prefill launch
         of its own, as it is where Q is a sequence of layers; the layers of a stacked Q are one launch per mask where the plan
         allows it.  `marks`, if given, is three events recorded before the first prefill launch, after the last dense-causal one and after the last one."""
@@ -193,7 +194,10 @@ class PureKVPipeline:
         k_cmp, v_cmp = k[lo:hi], v[lo:hi]
         P.purekv_select_topk(self.c[len(self.scored) - 1], v_cmp, self.batch, self.budget, idx_out=self.idx,
                              ws=self.select_ws)
-        P.purekv_compact_kv(k_cmp, v_cmp, self.idx, self.batch, self.budget, k_out=self.k_c, v_out=self.v_c)
+        if pages is not None:
+            pages.store_prompt(k_cmp, v_cmp, self.idx, self.batch, self.budget)
+        else:
+            P.purekv_compact_kv(k_cmp, v_cmp, self.idx, self.batch, self.budget, k_out=self.k_c, v_out=self.v_c)
 
     def alloc_host_io(self):
         """Pinned host buffers for run_host: (q, k, v) inputs and (k_c, v_c, o_last) outputs."""

@@ -283,3 +283,81 @@ def test_nothing_is_written_around_the_outputs():
         P.purekv_decode_paged(q, kp, vp, table, lens, max_len=hint, out=guard[64:-64].view(3, 6, 64), lse=lse[8:-8].view(3, 6))
         assert (guard[:64] == 7).all() and (guard[-64:] == 7).all() and (lse[:8] == 7).all() and (lse[-8:] == 7).all()
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, (kp, vp)))
+
+
+def test_nothing_to_do():
+    c = pc.Cache(24, [], 2, 64, "bf16", spare_pages=2)
+    (kp, vp, table, lens), _ = c.cuda()
+    empty = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    assert P.purekv_decode_paged(empty, kp, vp, table, lens).shape == (0, 4, 64)
+    P.purekv_append_paged(empty[:, :2], empty[:, :2], kp, vp, table, lens)
+    cu = torch.zeros(1, dtype=torch.int32, device="cuda")
+    holder = type("H", (), dict(cu_seqlens=cu, cu_kept=cu))
+    P.purekv_compact_paged(empty[None, :, :2], empty[None, :, :2], torch.zeros((1, 2, 0), dtype=torch.int32, device="cuda"), holder, holder, kp[None], vp[None], table, lens)
+    assert P.purekv_poll_status(None) == 0
+
+
+def test_a_list_without_pages():
+    # no column in the table, and no page in the pool: every row is missing, nothing is read
+    q = queries(25, 2, 4, 64, "bf16").cuda()
+    lens = torch.tensor([3, 0], dtype=torch.int32, device="cuda")
+    for n_pages, columns in ((2, 0), (0, 2)):
+        pool = torch.zeros((n_pages, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+        for hint in (0, 3):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            out = P.purekv_decode_paged(q, pool, pool, torch.zeros((2, columns), dtype=torch.int32, device="cuda"), lens, max_len=hint, status=status)
+            assert status.item() == P.ERR_BAD_PAGE and (out[1] == 0).all()
+
+
+def test_pools_that_lie_in_one_tensor():
+    # K and V pages side by side, and a window of a larger pool
+    c = pc.Cache(26, [700, 33, 0, 1500], 4, 128, "bf16", 16)
+    q = queries(26, 4, 16, 128, "bf16")
+    both = torch.full((c.k.shape[0], 2, 16, 6, 128), float("nan"), dtype=torch.bfloat16)
+    both[:, 0, :, 1:5], both[:, 1, :, 1:5] = c.k, c.v
+    both = both.cuda()
+    (_, _, table, lens), _ = c.cuda()
+    lse = torch.empty((4, 16), device="cuda")
+    for hint in (0, 1500):
+        compare(c, q, P.purekv_decode_paged(q.cuda(), both[:, 0, :, 1:5], both[:, 1, :, 1:5], table, lens, max_len=hint, lse=lse), lse)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "fp32"])
+def test_uninitialised_workspaces(kind):
+    c = pc.Cache(27, [3000, 1, 0, 900], 2, 64, kind, 16)
+    q = queries(27, 4, 8, 64, kind)
+    (kp, vp, table, lens), sc = c.cuda()
+    need = P.purekv_decode_paged_ws_bytes(4, 0, 8, 2, 64, P.FP32 if kind == "fp32" else P.BF16)
+    lse = torch.empty((4, 8), device="cuda")
+    for fill in (0xff, 0x7f, 0x01):
+        ws = torch.full((need + 64,), fill, dtype=torch.uint8, device="cuda")
+        compare(c, q, P.purekv_decode_paged(q.cuda(), kp, vp, table, lens, lse=lse, ws=ws[:need], **sc), lse)
+        assert (ws[need:] == fill).all()
+    with pytest.raises(P.PureKVError) as e:
+        P.purekv_decode_paged(q.cuda(), kp, vp, table, lens, ws=torch.empty(100, dtype=torch.uint8, device="cuda"), **sc)
+    assert e.value.status == P.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("hint", [0, 2000])
+def test_two_graphs_that_share_a_workspace(hint):
+    made = []
+    ws = torch.empty(P.purekv_decode_paged_ws_bytes(4, 0, 8, 2, 128), dtype=torch.uint8, device="cuda")
+    for seed, lens in ((28, [2000, 7, 0, 1000]), (29, [5, 1999, 300, 64])):
+        c = pc.Cache(seed, lens, 2, 128, "bf16", 16)
+        q = queries(seed, 4, 8, 128, "bf16")
+        (kp, vp, table, seq), _ = c.cuda()
+        dq, lse, out = q.cuda(), torch.empty((4, 8), device="cuda"), torch.empty(q.shape, dtype=q.dtype, device="cuda")
+        call = lambda a=(dq, kp, vp, table, seq), o=out, z=lse: P.purekv_decode_paged(*a, max_len=hint, out=o, lse=z, ws=ws)
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        made.append((c, q, out, lse, graph, dq, kp, vp, table, seq))
+    for _ in range(3):
+        for m in made:
+            m[2].fill_(float("nan"))
+            m[4].replay()
+    torch.cuda.synchronize()
+    for m in made:
+        compare(m[0], m[1], m[2], m[3])
