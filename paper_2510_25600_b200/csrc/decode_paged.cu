@@ -55,7 +55,8 @@ constexpr int kDpGroups = 128;   // of requests: their running sums of tiles lie
 constexpr int kDpSteals = 8;     // answers to requests for runs that a CTA keeps: more than runs its loads can be ahead of its products
 // Three quarters of a CTA's share of the tiles make its long run; the rest is cut into short runs, three for every CTA at work, of four
 // tiles at least, which go to whichever CTA asks next.
-constexpr int kDpShorts = 3, kDpShortest = 4;
+// Up to eight tiles per CTA all go into long runs: short ones would be as long as those.
+constexpr int kDpShorts = 3, kDpShortest = 4, kDpFew = 8;
 
 // Tiles of one head: `left` of them, from tile `tile` of request r (n rows) on, tile `at` of the head's.
 struct DpRun {
@@ -701,7 +702,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 #pragma unroll
     for (int x = 0; x < kPer; ++x) s_tiles[tid * kPer + x] = upto - sum + mine[x];
     __syncthreads();
-    long_tiles = min(all, max((int64_t)1, all * a.v_heads * 3 / 4 / a.at_once));
+    long_tiles = all * a.v_heads <= kDpFew * a.at_once ? (all + a.n_long - 1) / a.n_long : min(all, max((int64_t)1, all * a.v_heads * 3 / 4 / a.at_once));
     short_tiles = max((int64_t)kDpShortest, (max((int64_t)0, all - a.n_long * long_tiles) + a.n_short - 1) / a.n_short);
     if (tid == 0) chains[blockIdx.x].parts = 0;
     run = take(blockIdx.x);
@@ -1027,37 +1028,47 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (C == 1) return;
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    // four threads per output value, each over every fourth CTA's share (nh * cols * 4 is a multiple of 16: whole quarters)
-    const int32_t cols = D / C, part = tid & 3;
+    // four threads per four output values, each over every fourth CTA's share
+    const int32_t quads = D / C / 4, part = tid & 3, items = nh * quads * 4;
     const float vs = a.v_scale ? a.v_scale[g] : 1.f;
-    for (int32_t x0 = 0; x0 < nh * cols * 4; x0 += kThreads) {
-      const int32_t x = x0 + tid, y = min(x, nh * cols * 4 - 1), h = (y >> 2) / cols, c = (y >> 2) % cols;
-      float top = -INFINITY;
+    for (int32_t x0 = 0; x0 < items; x0 += kThreads) {
+      const int32_t x = x0 + tid, y = min(x, items - 1), h = (y >> 2) / quads, c = (y >> 2) % quads;
+      float mi[kDpClusterMax / 4], li[kDpClusterMax / 4], top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < kDpClusterMax / 4; ++k) {
         const int32_t j = part + 4 * k;
-        if (j < C) top = fmaxf(top, dp_seen(s_pml[j][h][0], s_pml[j][h][1]));
+        const float2 ml = j < C ? *reinterpret_cast<const float2*>(s_pml[j][h]) : make_float2(0.f, 0.f);
+        mi[k] = ml.x;
+        li[k] = ml.y;
+        top = fmaxf(top, dp_seen(ml.x, ml.y));
       }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float ref = dp_finite(top);
-      float acc = 0.f, l = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.f;
 #pragma unroll
       for (int k = 0; k < kDpClusterMax / 4; ++k) {
         const int32_t j = part + 4 * k;
         if (j < C) {
-          const float wgt = dp_weight(s_pml[j][h][0], s_pml[j][h][1], ref);
-          acc = fmaf(wgt, s_part[(j * nh + h) * cols + c], acc);
-          l = fmaf(wgt, s_pml[j][h][1], l);
+          const float wgt = dp_weight(mi[k], li[k], ref);
+          const float4 v = *reinterpret_cast<const float4*>(s_part + ((j * nh + h) * quads + c) * 4);
+          acc.x = fmaf(wgt, v.x, acc.x); acc.y = fmaf(wgt, v.y, acc.y); acc.z = fmaf(wgt, v.z, acc.z); acc.w = fmaf(wgt, v.w, acc.w);
+          l = fmaf(wgt, li[k], l);
         }
       }
-      acc += __shfl_xor_sync(0xffffffffu, acc, 1);
-      l += __shfl_xor_sync(0xffffffffu, l, 1);
-      acc += __shfl_xor_sync(0xffffffffu, acc, 2);
-      l += __shfl_xor_sync(0xffffffffu, l, 2);
-      if (part == 0 && x < nh * cols * 4) {
+#pragma unroll
+      for (int d = 1; d <= 2; d *= 2) {
+        acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d);
+        acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
+        acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d);
+        acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
+        l += __shfl_xor_sync(0xffffffffu, l, d);
+      }
+      if (part == 0 && x < items) {
         const int64_t hq = (int64_t)run.r * a.n_q_heads + h0 + h;
-        reinterpret_cast<Out*>(a.o)[hq * D + rank * cols + c] = (Out)(run.n > 0 ? acc * (vs / l) : 0.f);
+        const float inv = run.n > 0 ? vs / l : 0.f;
+        dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + (rank * quads + c) * 4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
         if (rank == 0 && c == 0 && a.lse) a.lse[hq] = run.n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
     }
@@ -1242,25 +1253,30 @@ struct DpForm {
 };
 // Measured over 1-128 requests of 16-64 000 rows, 4 and 2 KV heads, all three types (us).  A CTA alone on its SM streams 75 GB/s, all
 // together 6.3 TB/s; the even form costs 4 us besides, the balanced one 14.  Clusters: as many CTAs as find an SM each (128, or 64 for
-// clusters of eight and more: 4 requests of 1000 bf16 rows 7.8 with 4 CTAs each, 10.4 with 8), but not for less than 150 KB of
-// a head's rows (200 bf16 rows: 4.7 with one CTA, 5.4 with 16; 500: 7.3 and 5.4), and no pairs for less than 512 KB (64 heads of 500
-// rows: 7.8 alone, 9.3 in pairs).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all requests are as
-// long as the longest, but nothing says so (128 of 2900-5100 rows: 170 against 180; one of 60 000 among 63 of 100-2000: 57 against 450), and
-// where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
-static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int64_t row_bytes, int32_t at_once) {
+// clusters of eight and more: 8 requests of 1200 bf16 rows 7.7 with 4 CTAs each, 16 with 8), but not for less than 130 KB of
+// a head's rows (200 bf16 rows: 4.7 with one CTA, 5.0 with 4; 500: 7.3 and 5.1), and no pairs for less than 200 KB (64 heads of 300
+// rows: 6.2 alone, 6.9 in pairs; of 500 7.8 and 6.9).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all
+// requests are as long as the longest, but nothing says so (128 of 2900-5100 rows: 170 against 180; one of 60 000 among 63 of 100-2000: 57
+// against 450), and where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
+static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t head_dim, purekv_dtype held, int32_t at_once) {
+  const int64_t row_bytes = 2 * head_dim * bytes_of(held);
   const int64_t base = n_req * v_heads, bytes = longest * row_bytes;  // of one head's rows
   int32_t c = 1;
-  if (bytes > 150000) {
+  if (bytes > 130000) {
     while (c < kDpClusterMax && longest > 64 * c && base * 2 * c <= (c < 4 ? 128 : 64)) c *= 2;
-    if (c == 2 && bytes <= 512000) c = 1;
+    if (c == 2 && bytes <= 200000) c = 1;
   }
   const double all = (double)base * bytes / 6.3e6, share = (double)((base * c + 147) / 148) * bytes / c / 75e3;
   if (all < 60. && std::max(all, share) + 4. < all + 14.) {
-    // more heads than SMs: several CTAs of four warps on each, so that one streams while another starts or ends
-    const int32_t per_sm = base <= 148 || longest > 2048 ? 1 : longest > 64 ? 2 : 3;
+    // more heads than SMs: several CTAs of four warps on each, so that one streams while another starts or ends (128 requests of 500
+    // bf16 rows: 27 us, 33 with eight warps; e4m3 takes more warps than that: 29 and 27)
+    const int32_t few = held == PUREKV_E4M3 ? 128 : 2048;
+    const int32_t per_sm = base <= 148 || longest > few ? 1 : longest > 64 ? 2 : 3;
     return {c, 0, 0, 0, per_sm};
   }
-  return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((kDpShorts * at_once + v_heads - 1) / v_heads)};
+  // (no short runs, but one to be at hand, where the longest requests to be expected would not make any)
+  const int64_t shorts = longest < INT32_MAX && n_req * ((longest + 63) / 64) * v_heads <= kDpFew * at_once ? v_heads : kDpShorts * at_once;
+  return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((shorts + v_heads - 1) / v_heads)};
 }
 
 // The pools for the copy engine; false where it cannot take them.
@@ -1328,7 +1344,7 @@ size_t purekv_decode_paged_ws_bytes(int32_t n_req, int32_t max_len, int32_t n_q_
   // (of the pools' types that go with dtype, e4m3 has the shorter rows: either may need the larger workspace)
   const int64_t longest = max_len > 0 ? max_len : INT32_MAX;
   auto need = [&](purekv_dtype held) {
-    const DpForm f = dp_form(n_req, v_heads, longest, 2 * head_dim * bytes_of(held), dp_at_once(rows, held));
+    const DpForm f = dp_form(n_req, v_heads, longest, head_dim, held, dp_at_once(rows, held));
     return dp_ws(f, v_heads, group, head_dim, dtype);
   };
   return (size_t)std::max(need(dtype), dtype == PUREKV_FP32 ? 0 : need(PUREKV_E4M3));
@@ -1373,7 +1389,7 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
   a.o = o;
   a.lse = lse;
   a.status = status;
-  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX, 2 * pages->head_dim * bytes_of(pages->dtype),
+  const DpForm form = dp_form(a.n_req, a.v_heads, max_len > 0 ? max_len : INT32_MAX, pages->head_dim, pages->dtype,
                               dp_at_once(rows, pages->dtype));
   if (!form.cluster) {
     PK_REQUIRE(ws && ws_bytes >= (size_t)dp_ws(form, a.v_heads, a.group, pages->head_dim, dtype), PUREKV_ERR_WORKSPACE,
