@@ -1249,7 +1249,7 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
 // head.
 struct DpForm {
   int32_t cluster, at_once, n_long, n_short;
-  int32_t per_sm = 1;  // even form: CTAs per SM, of eight warps (1) or four (2, and 3 with a ring of one stage)
+  int32_t per_sm = 1;  // even form, CTAs of a head: 1 alone on its SM; 2 of four warps, two or three per SM; with rings of one stage 3 of four, 4 of eight
 };
 // Measured over 1-128 requests of 16-64 000 rows, 4 and 2 KV heads, all three types (us).  A CTA alone on its SM streams 75 GB/s, all
 // together 6.3 TB/s; the even form costs 4 us besides, the balanced one 14.  Clusters: as many CTAs as find an SM each (128, or 64 for
@@ -1268,10 +1268,11 @@ static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t h
   }
   const double all = (double)base * bytes / 6.3e6, share = (double)((base * c + 147) / 148) * bytes / c / 75e3;
   if (all < 60. && std::max(all, share) + 4. < all + 14.) {
-    // more heads than SMs: several CTAs of four warps on each, so that one streams while another starts or ends (128 requests of 500
-    // bf16 rows: 27 us, 33 with eight warps; e4m3 takes more warps than that: 29 and 27)
-    const int32_t few = held == PUREKV_E4M3 ? 128 : 2048;
-    const int32_t per_sm = base <= 148 || longest > few ? 1 : longest > 64 ? 2 : 3;
+    // more heads than SMs: several CTAs on each, so that one streams while another starts or ends.  Requests of one trip of four warps,
+    // or of eight, take rings of one stage (4, e4m3 8 KV heads, us, against eight warps with a ring of three: 128 requests of 100-200 rows 19
+    // and 28); others two or three CTAs of four warps (128 requests of 300-500 bf16 rows 25 and 32, e4m3 18 and 26).
+    const int32_t one_trip = held == PUREKV_E4M3 ? 256 : 128;
+    const int32_t per_sm = base <= 148 ? 1 : longest <= 64 ? 3 : longest <= one_trip && held != PUREKV_FP32 ? 4 : longest > 2048 ? 1 : 2;
     return {c, 0, 0, 0, per_sm};
   }
   // (no short runs, but one to be at hand, where the longest requests to be expected would not make any)
@@ -1309,7 +1310,8 @@ template <class E, class X, int ST8, int ST4, int OCC4>
 static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
   const bool whole = a.view.page_size.d % E::TK == 0;
   if (f.cluster && f.per_sm == 3) return launch_even<E, 4, 1, kDpRows, (E::R > 8 ? 2 : 3)>(a, f.cluster, stream);
-  if (f.cluster && f.per_sm == 2) return launch_even<E, 4, 3, kDpRows, 2>(a, f.cluster, stream);
+  if (f.cluster && f.per_sm == 4) return launch_even<E, 8, 1, kDpRows, (E::R > 8 ? 1 : 2)>(a, f.cluster, stream);
+  if (f.cluster && f.per_sm == 2) return launch_even<E, 4, (OCC4 == 3 ? 2 : 3), kDpRows, OCC4>(a, f.cluster, stream);
   if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
   DpMaps maps = {};
   if (dp_maps<X>(a, n_kv_heads, &maps)) return launch_balanced<X, 4, ST4, kDpEngine, OCC4>(a, maps, stream);

@@ -88,6 +88,27 @@ def test_many_requests():
     check(6, torch.randint(0, 300, (150,), generator=g).tolist(), 4, 4, 128, "e4m3", 16)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "e4m3"])
+@pytest.mark.parametrize("H,hkv,d,page", [(8, 2, 128, 16), (24, 2, 64, 7)])
+def test_every_way_of_launching(kind, H, hkv, d, page):
+    """What is expected to be the longest request sizes the launch, whatever the lengths are: few and many requests, each form of both."""
+    g = torch.Generator().manual_seed(30)
+    for lens in (torch.randint(0, 300, (80,), generator=g).tolist(), [700, 0, 3, 64], [129]):
+        c = pc.Cache(30, lens, hkv, d, kind, page)
+        q = queries(30, len(lens), H, d, kind)
+        (kp, vp, table, seq_lens), sc = c.cuda()
+        dq, lse = q.cuda(), torch.empty((len(lens), H), device="cuda")
+        want = None
+        for hint in (0, 1, 64, 65, 128, 129, 256, 257, 600, 2048, 2049, 9000, 1 << 17, (1 << 31) - 1):
+            got = P.purekv_decode_paged(dq, kp, vp, table, seq_lens, max_len=hint, out=torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda"), lse=lse.fill_(float("nan")), **sc)
+            if want is None:
+                want = got.float()
+                compare(c, q, got, lse)
+            else:                                  # two results within the tolerance of the same: compared with twice the weights' bound
+                assert ((got.float() - want).abs() <= 2.0 ** -6 * want.abs() + 2.0 ** -6).all(), hint
+        compare(c, q, got, lse)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 13, 21, 40, 70, 110])
 def test_lengths_one_by_one(n):
     check(7, list(range(n, n + 8)), 5, 1, 128, "bf16", 8, max_len=0)
