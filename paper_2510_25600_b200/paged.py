@@ -49,7 +49,10 @@ class PagedCache:
 
     def set_rows(self, rows: Sequence[int]) -> None:
         """Conversation r has rows[r] rows from now on (fewer than before give pages back); conversations past the end of `rows` keep
-        theirs.  All or nothing: without enough free pages, RuntimeError, and nothing changes."""
+        theirs.  All or nothing: without enough free pages, RuntimeError, and nothing changes.  Not in a graph's capture, which would
+        replay the lengths and pages of the capture."""
+        if self.on_gpu and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the rows of a paged cache are set outside of a graph's capture")
         if len(rows) > len(self._pages) or any(n < 0 or n > self.max_rows for n in rows):
             raise ValueError(f"up to {len(self._pages)} conversations of 0 to {self.max_rows} rows, got {list(rows)}")
         want = [-(-int(n) // self.page_size) for n in rows]
@@ -67,7 +70,7 @@ class PagedCache:
 
     def advance(self, new: int | Sequence[int] = 1) -> None:
         """Room for `new` more rows: so many for every conversation that has rows, or as many for each as given."""
-        if isinstance(new, int):
+        if np.ndim(new) == 0:
             new = np.where(self.h_lens > 0, new, 0)
         self.set_rows(self.h_lens[:len(new)] + np.asarray(new))
 
@@ -91,14 +94,19 @@ class PagedCache:
         self._dev.copy_(slot[0], non_blocking=True)
         if self.on_gpu:
             slot[1] = slot[1] or torch.cuda.Event()
-            slot[1].record()
+            slot[1].record(torch.cuda.current_stream(self._dev.device))
 
     def store_prompt(self, k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, batch: P.Batch, budget: P.Budget) -> None:
         """The rows `idx` keeps of the prompts' K and V [n_layers,T,H_kv,d], behind what the first batch.n_req conversations have."""
         n = batch.n_req
-        self.set_rows(self.h_lens[:n] + np.diff(budget.h_cu_kept))
-        P.purekv_compact_paged(k, v, idx, batch, budget, self.k, self.v, self.block_table[:n], self.seq_lens[:n], k_scale=self.k_scale,
-                               v_scale=self.v_scale, status=self.status)
+        before = self.h_lens[:n].copy()
+        self.set_rows(before + np.diff(budget.h_cu_kept))
+        try:
+            P.purekv_compact_paged(k, v, idx, batch, budget, self.k, self.v, self.block_table[:n], self.seq_lens[:n], k_scale=self.k_scale,
+                                   v_scale=self.v_scale, status=self.status)
+        except BaseException:
+            self.set_rows(before)  # no rows without a prompt in them
+            raise
 
     def _layer(self, layer: int) -> dict:
         return dict(k_scale=None if self.k_scale is None else self.k_scale[layer],

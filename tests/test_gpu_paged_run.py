@@ -159,3 +159,18 @@ def test_the_packed_cache_and_the_pages_agree():
         b = cache.attend(layer, q)
         for r in (0, 2):                   # request 1 has rows of its own in the pages
             assert (a[r].float() - b[r].float()).abs().max() <= 2.0 ** -6      # two bf16 results of values below 4: each within 2^-7
+
+
+def test_rows_are_not_set_in_a_capture():
+    cache = PagedCache(1, 8, 16, 2, 64, torch.bfloat16, 2, 40)
+    cache.set_rows([3, 17])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        torch.zeros(4, device="cuda")
+        with pytest.raises(RuntimeError):
+            cache.advance()
+    assert cache.h_lens.tolist() == [3, 17] and cache.free_pages == 5
+    cache.advance()
+    torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == [4, 18]

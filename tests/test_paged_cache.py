@@ -1,4 +1,6 @@
 """PagedCache hands every page to one conversation at a time, and takes all of a step's pages or none."""
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 import torch
@@ -29,6 +31,8 @@ def test_rows_come_and_go():
     assert c.h_lens.tolist() == [6, 0, 5] and c._pages[0] == first and c.free_pages == 6
     c.advance([3, 8])
     consistent(c)
+    c.advance(np.int64(0))
+    consistent(c)
     assert c.h_lens.tolist() == [9, 8, 5]
     c.release(0)
     consistent(c)
@@ -53,6 +57,20 @@ def test_all_or_nothing():
     assert before == ([list(p) for p in c._pages], c.h_lens.tolist(), list(c._free))
     consistent(c)
     c.set_rows([4, 8, 16])           # pages given back in the same step are there to be taken
+    consistent(c)
+
+
+def test_a_refused_prompt_takes_no_rows():
+    c = cache()
+    c.set_rows([5, 0, 4])
+    before = c.h_lens.tolist(), c.free_pages
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32)
+    batch = SimpleNamespace(n_req=2, cu_seqlens=ints(0, 6, 12))
+    budget = SimpleNamespace(h_cu_kept=np.array([0, 3, 7]), cu_kept=ints(0, 3, 7))
+    k = torch.zeros((2, 12, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):  # not on a GPU
+        c.store_prompt(k, k, torch.zeros((2, 1, 7), dtype=torch.int32), batch, budget)
+    assert before == (c.h_lens.tolist(), c.free_pages)
     consistent(c)
 
 
