@@ -81,8 +81,9 @@ __device__ __forceinline__ uint32_t dp_transpose(uint32_t x) {
 }
 // NT column tiles (of eight heads) and MT row tiles (of 16 keys): references, sums and weights.  sc[..][0, 1]: key g8, heads 2t and 2t + 1
 // of the lane's g8 = lane / 4, t = lane % 4; [2, 3]: key g8 + 8.  Before: logits in log2 units, -inf for keys that are not there; after:
-// the weights.  Returns whether O has to be multiplied by alpha.
-template <int MT, int NT>
+// the weights.  Returns whether O has to be multiplied by alpha.  The reference lies UP below the largest logit, so that weights go up to
+// 2^UP (references and sums go together, so nobody else has to know).
+template <int UP, int MT, int NT>
 __device__ __forceinline__ bool dp_softmax(float (&sc)[MT][NT][4], float (&m)[NT][2], float (&l)[NT][2], float (&alpha)[NT][2]) {
   bool grew = false;
 #pragma unroll
@@ -95,6 +96,7 @@ __device__ __forceinline__ bool dp_softmax(float (&sc)[MT][NT][4], float (&m)[NT
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+      if constexpr (UP > 0) mx -= (float)UP;
       const bool up = mx > m[nt][x];
       alpha[nt][x] = up ? dec_ex2(m[nt][x] - mx) : 1.f;
       m[nt][x] = up ? mx : m[nt][x];
@@ -217,7 +219,7 @@ struct Bf16Rows {
         for (int x = 0; x < 4; ++x)
           sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? (sc[mt][nt][x] + odd[mt][nt][x]) * unit : -INFINITY;
     float alpha[NT][2];
-    if (dp_softmax<MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
+    if (dp_softmax<0, MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       uint32_t p[NT][2];
@@ -249,8 +251,9 @@ struct Bf16Rows {
 };
 
 // e4m3 pools: every e4m3 number is an fp16 number, so the tiles are fp16 with exact keys and values; the queries' rows are brought into
-// fp16's range by a power of two each, and the weights, at most 1, lose less in fp16 than in bf16.  The scale of the keys goes into the
-// logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
+// fp16's range by a power of two each.  The weights go up to 2^15 (fp16 ends at 65504): they keep 11 bits down to 2^-29 of the largest
+// and are off by 2^-40 of it at most below, so that not even a million keys of 2^-26 are lost, as they would be with weights up to 1.  The
+// scale of the keys goes into the logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
 // terms is free, so the queries' fragments are laid out to match.  Of the values, ldmatrix transposes pairs of bytes: a register
 // holds two columns of two keys, which go to two tiles, of the even columns and of the odd ones.
 template <int D_, int NT, int MT, bool SW_>
@@ -262,6 +265,7 @@ struct E4m3Rows {
   using VAt = RowsAt<TK, RowBytes, VS, SW>;
   using Out = __nv_bfloat16;
   struct Shared {};
+  static constexpr int kUp = 15;
   uint32_t qb[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2], unit[NT][2];
 
@@ -353,7 +357,7 @@ struct E4m3Rows {
 #pragma unroll
         for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
     float alpha[NT][2];
-    if (dp_softmax<MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
+    if (dp_softmax<kUp, MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       uint32_t p[NT][2];

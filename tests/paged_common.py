@@ -83,10 +83,10 @@ def attention(q, k, v, scale=None):
 def attention_tolerance(dtype, kind, o, weight, size, d):
     """A logit is a sum of d products in 32 bits: off by at most (d + 2) 2^-24 of the sum of its terms' sizes (`size`), and the
     scale's roundings, 4 more of them; the weights are off by that much, relatively, in the numerator and again in the sum, and by the
-    exponential's 2^-21.  A weight is rounded to bf16 (half a step, 2^-8) for bf16 pools and to fp16 (2^-11, or 2^-25 of the largest
-    weight where it is subnormal; a head has fewer than 2^14 keys here, so 2^-11 of their sum) for e4m3 ones.  O is rounded once."""
+    exponential's 2^-21.  A weight is rounded to bf16 (half a step, 2^-8) for bf16 pools and to fp16 (2^-11, or 2^-40 of the largest
+    weight below 2^-29 of it; a head has fewer than 2^14 keys here, so 2^-26 of their sum) for e4m3 ones.  O is rounded once."""
     logits = 2.0 * ((d + 6) * 2.0 ** -24 * size[:, None] + 2.0 ** -21)
-    weights = {"bf16": 2.0 ** -8, "e4m3": 2.0 ** -10, "fp32": 0.0}[kind]
+    weights = {"bf16": 2.0 ** -8, "e4m3": 2.0 ** -11 + 2.0 ** -26, "fp32": 0.0}[kind]
     sums = 2.0 ** -16  # 32-bit sums over the keys, warps and parts
     return weight * (logits + weights + sums) + HALF_STEP[dtype] * o.abs() * 1.02 + 1e-30
 

@@ -109,6 +109,22 @@ def test_every_way_of_launching(kind, H, hkv, d, page):
         compare(c, q, got, lse)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "e4m3"])
+@pytest.mark.parametrize("d,n", [(64, 40), (128, 3000)])
+def test_many_keys_of_little_weight(kind, d, n):
+    # one key has nearly all the weight, its values are 0: what comes out is the others', of 2^-26 of its weight each
+    c = pc.Cache(31, [n, 1], 2, d, kind, scales=False)
+    q = torch.ones((2, 8, d), dtype=torch.float32 if kind == "fp32" else torch.bfloat16)
+    for s in range(n):
+        c.k[c.table[0, s // c.page], s % c.page] = torch.tensor(2.25 if s == 7 else 0.0).to(c.k.dtype)
+        c.v[c.table[0, s // c.page], s % c.page] = torch.tensor(0.0 if s == 7 else 448.0).to(c.v.dtype)
+    (kp, vp, table, lens), sc = c.cuda()
+    lse = torch.empty((2, 8), device="cuda")
+    for hint in (0, 1, n, 9000):
+        got = P.purekv_decode_paged(q.cuda(), kp, vp, table, lens, max_len=hint, lse=lse, softmax_scale=8.0 / d, **sc)
+        compare(c, q, got, lse, 8.0 / d)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 13, 21, 40, 70, 110])
 def test_lengths_one_by_one(n):
     check(7, list(range(n, n + 8)), 5, 1, 128, "bf16", 8, max_len=0)
