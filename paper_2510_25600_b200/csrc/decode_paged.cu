@@ -1080,13 +1080,12 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 }
 
 // Joins the parts of the requests that cuts went through: grid (runs / J, heads of a tile / HPB).  A block looks after J runs' chains, one
-// after the other, and HPB heads of each: D / 4 threads per head, and as many groups of those as 256 threads hold.  A group takes eight or
-// sixteen parts at a time, all loads of which are asked for before the first is used, and runs a softmax of its own over them; the groups meet in
-// shared memory.  Many chains of few parts: a block each, all heads (J 1, HPB 8).  Few chains, of many parts: a head each (J 8, HPB 1).
-// Requests without rows get their zeros here.
-template <typename Out, int D, int R, int HPB, int J>
-__global__ void __launch_bounds__(256) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
-  constexpr int kHead = D / 4, kGroup = HPB * kHead, kGroups = 256 / kGroup, kAtOnce = J == 1 ? 16 : 8;
+// after the other, and HPB heads of each: D / 4 threads per head, and as many groups of those as 256 threads hold.  A group takes AO parts
+// at a time, all loads of which are asked for before the first is used, and runs a softmax of its own over them; the groups meet in
+// shared memory.  OCC blocks per SM.  Requests without rows get their zeros here.
+template <typename Out, int D, int R, int HPB, int J, int AO, int OCC>
+__global__ void __launch_bounds__(256, OCC) decode_paged_join_kernel(const __grid_constant__ DecodePagedArgs a) {
+  constexpr int kHead = D / 4, kGroup = HPB * kHead, kGroups = 256 / kGroup, kAtOnce = AO;
   static_assert(kGroups >= 1, "a head's columns fit a block");
   __shared__ float s_ml[kGroups][HPB][2];
   __shared__ __align__(16) float4 s_acc[kGroups][kGroup];
@@ -1237,16 +1236,22 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
   const int32_t runs = a.v_heads * (a.n_long + a.n_short);
   DpLaunch l(dim3((unsigned)runs), W * 32, (size_t)W * dp_warp_bytes<E, ST>() + (LOAD == kDpEngine ? 1024 : 0), stream);
   PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a, maps));
-  // (segments that cuts can go through: requests x heads; 16 parts each on average at the limit)
-  constexpr int kWide = E::R < 8 ? E::R : 8;
-  const bool many = (int64_t)a.n_req * a.v_heads * 16 >= runs;
+  // What cuts can go through are segments, a request's tiles of one head.  Short chains, of three or four parts, of many segments: a block
+  // each, all heads, few registers.  Longer ones: two heads and four chains a block.  Few, of very many parts: a head each.  Decode of 128
+  // requests of 2900-5100 rows, us, by these three: 164, 169, 182 (e4m3 168, 171, 184); one of 60 000 rows among 63 of 100-2000: 61, 58, 65; two of
+  // 150-250 thousand: 250, 236, 235.
+  const int64_t segments = (int64_t)a.n_req * a.v_heads;
   const int32_t heads = std::min(E::R, a.group);
-  DpLaunch j(many ? dim3((unsigned)runs, (unsigned)((heads + kWide - 1) / kWide)) : dim3((unsigned)((runs + 7) / 8), (unsigned)heads), 256, 0, stream);
-  if (many)
-    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<typename E::Out, E::D, E::R, kWide, 1>, a));
-  else
-    PK_CUDA(cudaLaunchKernelEx(&j.cfg, decode_paged_join_kernel<typename E::Out, E::D, E::R, 1, 8>, a));
-  return PUREKV_OK;
+  auto join = [&](auto kernel, int32_t chains, int32_t heads_each) -> purekv_status {
+    DpLaunch j(dim3((unsigned)((runs + chains - 1) / chains), (unsigned)((heads + heads_each - 1) / heads_each)), 256, 0, stream);
+    PK_CUDA(cudaLaunchKernelEx(&j.cfg, kernel, a));
+    return PUREKV_OK;
+  };
+  using Out = typename E::Out;
+  constexpr int kWide = E::R < 8 ? E::R : 8;
+  if (segments * 3 >= runs) return join(decode_paged_join_kernel<Out, E::D, E::R, kWide, 1, 4, 4>, 1, kWide);
+  if (segments * 16 >= runs) return join(decode_paged_join_kernel<Out, E::D, E::R, 2, 4, 4, 4>, 4, 2);
+  return join(decode_paged_join_kernel<Out, E::D, E::R, 1, 8, 8, 1>, 8, 1);
 }
 
 // How a call is launched: C CTAs per (request, head) in a cluster, or, with 0, the balanced form with so many long and short runs of a
