@@ -253,9 +253,12 @@ struct Bf16Rows {
 // e4m3 pools: every e4m3 number is an fp16 number, so the tiles are fp16 with exact keys and values; the queries' rows are brought into
 // fp16's range by a power of two each.  The weights go up to 2^15 (fp16 ends at 65504): they keep 11 bits down to 2^-29 of the largest
 // and are off by 2^-40 of it at most below, so that not even a million keys of 2^-26 are lost, as they would be with weights up to 1.  The
-// scale of the keys goes into the logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once: the order in which a dot product takes its
-// terms is free, so the queries' fragments are laid out to match.  Of the values, ldmatrix transposes pairs of bytes: a register
-// holds two columns of two keys, which go to two tiles, of the even columns and of the odd ones.
+// scale of the keys goes into the logits' factor, that of the values into the output.  A lane reads 16 bytes of a key at once:
+// the order in which a dot product takes its terms is free, so the queries' fragments are laid out to match.  Of the values,
+// ldmatrix transposes 16 x 16 bytes: a register holds a column of four keys, whose halves are two registers of a tile of V^T once they
+// are fp16; the keys' rows in the tiles of logits are in the order that this gives.  (Transposed in pairs of bytes, and the columns sorted
+// out after the conversion, it is a quarter more instructions, which set the pace under the power cap: 128 requests of 2900-5100 rows, 8 KV
+// heads, call after call at 1640 MHz, 181 us against 174.)
 template <int D_, int NT, int MT, bool SW_>
 struct E4m3Rows {
   static constexpr bool SW = SW_;
@@ -269,6 +272,8 @@ struct E4m3Rows {
   uint32_t qb[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2], unit[NT][2];
 
+  // The key of 16 in row g8 (x 0) or g8 + 8 (x 1) of a tile of logits.
+  static __device__ __forceinline__ int key(int g8, int x) { return 4 * (g8 >> 1) + (g8 & 1) + 2 * x; }
   static __device__ __forceinline__ uint32_t half2_of(uint16_t pair) {
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(pair));
@@ -336,12 +341,12 @@ struct E4m3Rows {
     for (int j = 0; j < CL; ++j)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        uint32_t w[2][4];  // keys g8 and g8 + 8
+        uint32_t w[2][4];  // the keys of rows g8 and g8 + 8 of the tile
 #pragma unroll
         for (int x = 0; x < 2; ++x)
           asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                        : "=r"(w[x][0]), "=r"(w[x][1]), "=r"(w[x][2]), "=r"(w[x][3])
-                       : "r"(KAt::at(st, 16 * mt + 8 * x + g8, CL * t + j)) : "memory");
+                       : "r"(KAt::at(st, 16 * mt + key(g8, x), CL * t + j)) : "memory");
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const uint32_t a0 = half2_of((uint16_t)w[0][s]), a2 = half2_of((uint16_t)(w[0][s] >> 16));
@@ -355,7 +360,7 @@ struct E4m3Rows {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + g8 + 8 * (x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
+        for (int x = 0; x < 4; ++x) sc[mt][nt][x] = mask >> (16 * mt + key(g8, x >> 1)) & 1 ? sc[mt][nt][x] * unit[nt][x & 1] : -INFINITY;
     float alpha[NT][2];
     if (dp_softmax<kUp, MT, NT>(sc, m, l, alpha)) dp_rescale(o, alpha);
 #pragma unroll
@@ -367,24 +372,17 @@ struct E4m3Rows {
         p[nt][1] = dp_transpose(pack_half(sc[mt][nt][2], sc[mt][nt][3]));
       }
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {  // 32 columns: b[0] and b[1] keys 2t, 2t + 1 and 2t + 8, 2t + 9 of the first 16, b[2] and b[3] of the others
-        uint32_t b[4], lo[4], hi[4];
-        dec_ldsm_t(VAt::at(st + TK * KS, 16 * mt + (lane & 7) + 8 * ((lane >> 3) & 1), 2 * c + (lane >> 4)), b);
+      for (int c = 0; c < D / 32; ++c) {  // 32 columns: r[0], r[1] columns g8 and g8 + 8 of keys 4t .. 4t + 3, r[2], r[3] the same of the other 16
+        uint32_t r[4];
+        asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(VAt::at(st + TK * KS, 16 * mt + (lane & 15), 2 * c + (lane >> 4))) : "memory");
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          lo[i] = half2_of((uint16_t)b[i]);
-          hi[i] = half2_of((uint16_t)(b[i] >> 16));
-        }
-        uint32_t even[4], odd[4];
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t a0 = half2_of((uint16_t)r[2 * y]), a2 = half2_of((uint16_t)(r[2 * y] >> 16));
+          const uint32_t a1 = half2_of((uint16_t)r[2 * y + 1]), a3 = half2_of((uint16_t)(r[2 * y + 1] >> 16));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          even[i] = __byte_perm(lo[i], hi[i], 0x5410);
-          odd[i] = __byte_perm(lo[i], hi[i], 0x7632);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma(o[2 * c][nt], even[0], even[2], even[1], even[3], p[nt][0], p[nt][1]);
-          mma(o[2 * c + 1][nt], odd[0], odd[2], odd[1], odd[3], p[nt][0], p[nt][1]);
+          for (int nt = 0; nt < NT; ++nt) mma(o[2 * c + y][nt], a0, a1, a2, a3, p[nt][0], p[nt][1]);
         }
       }
     }
@@ -396,10 +394,9 @@ struct E4m3Rows {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c)
+      for (int n = 0; n < D / 16; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          *reinterpret_cast<float2*>(rows + (8 * nt + 2 * t + (x & 1)) * ld + 32 * c + 16 * (x >> 1) + 2 * g8) = make_float2(o[2 * c][nt][x], o[2 * c + 1][nt][x]);
+        for (int x = 0; x < 4; ++x) rows[(8 * nt + 2 * t + (x & 1)) * ld + 16 * n + g8 + 8 * (x >> 1)] = o[n][nt][x];
   }
 };
 
@@ -1331,7 +1328,7 @@ static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, c
 static int32_t dp_rows(int32_t group, purekv_dtype dtype) { return dtype == PUREKV_FP32 ? (group <= 2 ? 2 : 8) : group <= 8 ? 8 : 16; }
 
 // CTAs of the balanced form at work: two per SM, or three where the products and not the loads take the time: of e4m3, which has to
-// become fp16, with up to eight heads (128 requests of 2900-5100 rows, 8 KV heads, pages of 16 rows: 201 us with two, 176 with three; of 64 rows 185 and 183).
+// become fp16, with up to eight heads (128 requests of 2900-5100 rows, 8 KV heads, call after call under the power cap, us: pages of 16 rows 197 with two, 178 with three; of 64 rows 183 and 173).
 constexpr int dp_ctas(bool e4m3, int rows) { return e4m3 && rows == 8 ? 3 : 2; }
 static int32_t dp_at_once(int32_t rows, purekv_dtype held) { return 148 * dp_ctas(held == PUREKV_E4M3, rows); }
 
