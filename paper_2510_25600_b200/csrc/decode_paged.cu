@@ -574,6 +574,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   __shared__ __align__(8) float s_pml[CLUSTER ? kDpClusterMax : 1][R][2];  // every CTA's (reference, sum) per head
   __shared__ int64_t s_sum[W];
   __shared__ int64_t s_tiles[CLUSTER ? 1 : kDpGroups];                // running sums of the requests' tiles, by groups of requests
+  __shared__ int32_t s_rows[CLUSTER ? 1 : kDpGroups];                 // rows of the last request of each group
   __shared__ __align__(16) ulonglong2 s_stolen[CLUSTER ? 1 : kDpSteals];  // answers to this CTA's requests for runs
   __shared__ __align__(8) uint64_t s_answered[CLUSTER ? 1 : kDpSteals];
   __shared__ DpRun s_run[CLUSTER ? 1 : W][kDpSteals];                 // per warp: the runs that its loads have entered
@@ -614,6 +615,12 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       hit = __ballot_sync(0xffffffffu, lane < kDpGroups / 32 && s_tiles[first + lane % (kDpGroups / 32)] > x.at);
       const int32_t group = first + __ffs(hit) - 1, per_group = (a.n_req + kDpGroups - 1) / kDpGroups;
       int64_t before = group > 0 ? s_tiles[group - 1] : 0;
+      if (per_group == 1) {
+        x.r = group;
+        x.n = s_rows[group];
+        x.tile = (int32_t)(x.at - before);
+        return x;
+      }
       for (int32_t i0 = group * per_group; i0 < a.n_req; i0 += 32) {
         const int32_t rows = i0 + lane < a.n_req ? rows_of(i0 + lane) : 0;
         int64_t upto = tiles_of(rows);
@@ -684,7 +691,11 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 #pragma unroll
     for (int x = 0; x < kPer; ++x) {
       const int32_t i0 = (tid * kPer + x) * per_group;
-      for (int32_t i = i0; i < min(i0 + per_group, a.n_req); ++i) sum += tiles_of(rows_of(i));
+      for (int32_t i = i0; i < min(i0 + per_group, a.n_req); ++i) {
+        const int32_t rows = rows_of(i);
+        s_rows[tid * kPer + x] = rows;
+        sum += tiles_of(rows);
+      }
       mine[x] = sum;
     }
     int64_t upto = sum;
