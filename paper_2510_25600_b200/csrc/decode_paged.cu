@@ -1244,10 +1244,10 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
   const int32_t runs = a.v_heads * (a.n_long + a.n_short);
   DpLaunch l(dim3((unsigned)runs), W * 32, (size_t)W * dp_warp_bytes<E, ST>() + (LOAD == kDpEngine ? 1024 : 0), stream);
   PK_CUDA(cudaLaunchKernelEx(&l.cfg, kernel, a, maps));
-  // What cuts can go through are segments, a request's tiles of one head.  Short chains, of three or four parts, of many segments: a block
+  // What cuts can go through are segments, a request's tiles of one head.  Short chains, of up to five parts on average: a block
   // each, all heads, few registers.  Longer ones: two heads and four chains a block.  Few, of very many parts: a head each.  Decode of 128
-  // requests of 2900-5100 rows, us, by these three: 164, 169, 182 (e4m3 168, 171, 184); one of 60 000 rows among 63 of 100-2000: 61, 58, 65; two of
-  // 150-250 thousand: 250, 236, 235.
+  // requests of 2900-5100 rows, us, by these three: 164, 169, 182 (e4m3 168, 171, 184); one of 60 000 rows among 63 of 100-2000: 61, 58, 65; 128 of
+  // 2900-5100 with 4 heads in e4m3: 98, 103; two of 150-250 thousand: 250, 236, 235.
   const int64_t segments = (int64_t)a.n_req * a.v_heads;
   const int32_t heads = std::min(E::R, a.group);
   auto join = [&](auto kernel, int32_t chains, int32_t heads_each) -> purekv_status {
@@ -1257,7 +1257,7 @@ static purekv_status launch_balanced(const DecodePagedArgs& a, const DpMaps& map
   };
   using Out = typename E::Out;
   constexpr int kWide = E::R < 8 ? E::R : 8;
-  if (segments * 3 >= runs) return join(decode_paged_join_kernel<Out, E::D, E::R, kWide, 1, 4, 4>, 1, kWide);
+  if (segments * 4 >= runs) return join(decode_paged_join_kernel<Out, E::D, E::R, kWide, 1, 4, 4>, 1, kWide);
   if (segments * 16 >= runs) return join(decode_paged_join_kernel<Out, E::D, E::R, 2, 4, 4, 4>, 4, 2);
   return join(decode_paged_join_kernel<Out, E::D, E::R, 1, 8, 8, 1>, 8, 1);
 }
@@ -1273,7 +1273,7 @@ struct DpForm {
 // clusters of eight and more: 8 requests of 1200 bf16 rows 7.7 with 4 CTAs each, 16 with 8), but not for less than 130 KB of
 // a head's rows (200 bf16 rows: 4.7 with one CTA, 5.0 with 4; 500: 7.3 and 5.1), and no pairs for less than 200 KB (64 heads of 300
 // rows: 6.2 alone, 6.9 in pairs; of 500 7.8 and 6.9).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all
-// requests are as long as the longest, but nothing says so (128 of 2900-5100 rows: 170 against 180; one of 60 000 among 63 of 100-2000: 57
+// requests are as long as the longest, but nothing says so (128 of 2900-5100 rows: 167 against 173; one of 60 000 among 63 of 100-2000: 57
 // against 450), and where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
 static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t head_dim, purekv_dtype held, int32_t at_once) {
   const int64_t row_bytes = 2 * head_dim * bytes_of(held);
@@ -1286,8 +1286,8 @@ static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t h
   const double all = (double)base * bytes / 6.3e6, share = (double)((base * c + 147) / 148) * bytes / c / 75e3;
   if (all < 60. && std::max(all, share) + 4. < all + 14.) {
     // more heads than SMs: several CTAs on each, so that one streams while another starts or ends.  Requests of one trip of four warps,
-    // or of eight, take rings of one stage (4, e4m3 8 KV heads, us, against eight warps with a ring of three: 128 requests of 100-200 rows 19
-    // and 28); others two or three CTAs of four warps (128 requests of 300-500 bf16 rows 25 and 32, e4m3 18 and 26).
+    // or of eight, take rings of one stage (4, e4m3 8 KV heads, us, against eight warps with a ring of three: 128 requests of 100-200 rows 18
+    // and 28); others two or three CTAs of four warps (128 requests of 300-500 bf16 rows 25 and 30, e4m3 18 and 25).
     const int32_t one_trip = held == PUREKV_E4M3 ? 256 : 128;
     const int32_t per_sm = base <= 148 ? 1 : longest <= 64 ? 3 : longest <= one_trip && held != PUREKV_FP32 ? 4 : longest > 2048 ? 1 : 2;
     return {c, 0, 0, 0, per_sm};
