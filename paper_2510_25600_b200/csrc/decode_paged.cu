@@ -25,6 +25,7 @@
 #include "decode.cuh"
 #include "paged.cuh"
 #include "paged_args.cuh"
+#include "paged_runs.cuh"
 #include "tc_util.cuh"
 
 namespace purekv {
@@ -53,10 +54,7 @@ struct DecodePagedArgs {
 constexpr int kDpClusterMax = 16;
 constexpr int kDpGroups = 128;   // of requests: their running sums of tiles lie in shared memory
 constexpr int kDpSteals = 8;     // answers to requests for runs that a CTA keeps: more than runs its loads can be ahead of its products
-// Three quarters of a CTA's share of the tiles make its long run; the rest is cut into short runs, three for every CTA at work, of four
-// tiles at least, which go to whichever CTA asks next.
-// Up to eight tiles per CTA all go into long runs: short ones would be as long as those.
-constexpr int kDpShorts = 3, kDpShortest = 4, kDpFew = 8;
+constexpr int kDpShorts = 3;     // short runs for every CTA at work
 
 // Tiles of one head: `left` of them, from tile `tile` of request r (n rows) on, tile `at` of the head's.
 struct DpRun {
@@ -578,6 +576,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   __shared__ __align__(16) ulonglong2 s_stolen[CLUSTER ? 1 : kDpSteals];  // answers to this CTA's requests for runs
   __shared__ __align__(8) uint64_t s_answered[CLUSTER ? 1 : kDpSteals];
   __shared__ DpRun s_run[CLUSTER ? 1 : W][kDpSteals];                 // per warp: the runs that its loads have entered
+  __shared__ int32_t s_found[2];                                      // a run that one thread has found, and the answers it has read
 
   const int32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int32_t C = CLUSTER ? (int32_t)gridDim.x : 1, rank = CLUSTER ? (int32_t)blockIdx.x : 0;
@@ -599,15 +598,11 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 
   // The work at hand: `left` tiles from tile `tile` of (request r with n rows, virtual head vh) on.
   DpRun run = {};
-  int64_t all = 0, long_tiles = 0, short_tiles = 0;  // of a head: all tiles, those of a long and of a short run
-  // run b: of head b % v_heads the (b / v_heads)th, first the long ones
-  auto starts_at = [&](int32_t j) {
-    return min(all, j <= a.n_long ? j * long_tiles : a.n_long * long_tiles + (j - a.n_long) * short_tiles);
-  };
+  int32_t f_answers = 0;  // read so far
+  RunCuts cuts = {};
   auto take = [&](int32_t b) {
-    const int32_t j = b / a.v_heads;
-    DpRun x = {b, b - j * a.v_heads, 0, 0, 0, starts_at(j), 0};
-    x.left = starts_at(j + 1) - x.at;
+    const int32_t j = cuts.piece_of(b);
+    DpRun x = {b, b - j * a.v_heads, 0, 0, 0, cuts.starts_at(j), cuts.tiles(b)};
     if (x.left > 0) {
       // the group of requests in which tile x.at lies, then the request
       uint32_t hit = __ballot_sync(0xffffffffu, s_tiles[lane * (kDpGroups / 32) + kDpGroups / 32 - 1] > x.at);
@@ -666,13 +661,18 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     return yes ? (int32_t)b : -1;
   };
   ChainRecord* const chains = reinterpret_cast<ChainRecord*>(a.chains);
-  // Once a run is empty all further ones are: what no CTA has started need not be.
-  auto drain = [&](int32_t k) {
-    for (int32_t b = 0;; ++k) {
-      ask(k);
-      if ((b = answer(k)) < 0) return;
-      chains[b].parts = 0;
+  // The next run with tiles among those that no CTA has started, `k` answers having been read; without tiles if there are none.  One
+  // thread asks for the block: the answers' slots are its own as long as no warp waits for one.
+  auto find = [&](int32_t& k) {
+    if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again
+    if (tid == 0) {
+      s_found[0] = next_run(cuts, [&] { ask(k); return answer(k++); }, [&](int32_t b) { chains[b].parts = 0; });
+      s_found[1] = k;
     }
+    __syncthreads();
+    k = s_found[1];
+    const int32_t b = s_found[0];
+    return b < 0 ? DpRun{} : take(b);
   };
   if constexpr (CLUSTER) {
     run = {0, (int32_t)blockIdx.y, (int32_t)blockIdx.z, 0, rows_of(blockIdx.z), 0, 0};
@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
       mine[x] = sum;
     }
-    int64_t upto = sum;
+    int64_t upto = sum, all = 0;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
@@ -714,15 +714,14 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 #pragma unroll
     for (int x = 0; x < kPer; ++x) s_tiles[tid * kPer + x] = upto - sum + mine[x];
     __syncthreads();
-    long_tiles = all * a.v_heads <= kDpFew * a.at_once ? (all + a.n_long - 1) / a.n_long : min(all, max((int64_t)1, all * a.v_heads * 3 / 4 / a.at_once));
-    short_tiles = max((int64_t)kDpShortest, (max((int64_t)0, all - a.n_long * long_tiles) + a.n_short - 1) / a.n_short);
+    cuts = RunCuts::of(all, a.v_heads, a.at_once, a.n_long, a.n_short);
     if (tid == 0) chains[blockIdx.x].parts = 0;
     run = take(blockIdx.x);
     if (run.left <= 0) {
-      if (tid == 0) drain(0);
-      return;
+      run = find(f_answers);
+      if (run.left <= 0) return;
     }
-    if (tid == 0) ask(0);
+    if (tid == 0) ask(f_answers);
   }
 
   // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier).
@@ -743,8 +742,8 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
 
   // ---- loads.  The cursor runs ahead of the products, over the ends of requests and of runs.
   DpRun f = run;
-  int32_t f_answers = 0, f_runs = 1;  // answers read, runs entered
-  bool f_more = !CLUSTER, f_empty = false;
+  int32_t f_runs = 1;  // entered
+  bool f_more = !CLUSTER, f_empty = false;  // a further run is asked for; the last one asked for had no tiles
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dp_smem) + (uint32_t)warp * kWarpBytes;
   // The page of a row, its slot there and its KV head.  WHOLE: of the trip's first row, `there` of whose rows are wanted (copy engine:
   // of the first row of box `lane`, if there are several, and of that box); otherwise of row `lane` of the trip, `there` 1 if it is
@@ -883,16 +882,6 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (lane == 0) s_mask[warp][stage] = mask;
     if constexpr (LOAD != kDpEngine) asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
   };
-  Look next;
-  {
-    Look ahead[ST > 1 ? ST - 1 : 1];
-#pragma unroll
-    for (int s = 0; s < (ST > 1 ? ST - 1 : 1); ++s) ahead[s] = look();
-#pragma unroll
-    for (int s = 0; s < (ST > 1 ? ST - 1 : 1); ++s) fetch(s, ahead[s]);
-    next = look();
-  }
-
   E e;
   auto heads_at = [&](int32_t v, int32_t& g, int32_t& h0, int32_t& nh) {
     g = a.blocks == 1 ? v : v / a.blocks;
@@ -901,14 +890,24 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     nh = min(R, a.group - b * R);
   };
   int32_t g, h0, nh;
+  int32_t stage = 0, c_runs = 1;  // c_runs: runs entered by the products
+  uint32_t phase = 0;
+  bool from_start;  // whether this run has the request's first tile
+[[maybe_unused]] begin:
+  Look next;
+  {
+    Look ahead[ST > 1 ? ST - 1 : 1];
+#pragma unroll
+    for (int s = 0; s < (ST > 1 ? ST - 1 : 1); ++s) ahead[s] = look();
+#pragma unroll
+    for (int s = 0; s < (ST > 1 ? ST - 1 : 1); ++s) fetch(stage + s < ST ? stage + s : stage + s - ST, ahead[s]);
+    next = look();
+  }
   heads_at(run.vh, g, h0, nh);
   e.load(a, s_e, run.r, g, h0, nh);
   e.ready(s_e);
   __syncthreads();
-
-  int32_t stage = 0, c_runs = 1;  // c_runs: runs entered by the products
-  uint32_t phase = 0;
-  bool from_start = run.tile == 0;  // whether this run has the request's first tile
+  from_start = run.tile == 0;
   while (true) {
     bool end_of_request = true;
     if (run.left > 0) {
@@ -1019,9 +1018,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     } else {
       if (from_start && !end_of_request && tid == 0) {  // the first of several parts; the last is the run with the request's last tile
         const int64_t last = done.at - 1 + (tiles_of(done.n) - done.tile);
-        const int32_t j = done.id / a.v_heads;
-        const int32_t until = (int32_t)(last < a.n_long * long_tiles ? last / long_tiles : a.n_long + (last - a.n_long * long_tiles) / short_tiles);
-        chains[done.id] = {done.r, done.vh, until - j + 1, 0};
+        chains[done.id] = {done.r, done.vh, cuts.piece_with(last) - cuts.piece_of(done.id) + 1, 0};
       }
       if (!more) break;
       e.ready(s_e);
@@ -1033,7 +1030,19 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     }
   }
   if constexpr (!CLUSTER) {
-    if (f_empty && tid == 0) drain(f_answers);
+    // Runs without tiles are the last ones, but nothing says that CTAs start in that order: others may be left behind one.  They are
+    // begun as the first one was; the ring goes on where it is, a round later (its other stages were asked for nothing).
+    if (f_empty) {
+      run = find(f_answers);
+      if (run.left > 0) {
+        if (tid == 0) ask(f_answers);
+        f = run;
+        f_more = true;
+        f_empty = false;
+        phase ^= 1u;
+        goto begin;
+      }
+    }
   }
 
   if constexpr (CLUSTER) {
@@ -1293,7 +1302,7 @@ static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t h
     return {c, 0, 0, 0, per_sm};
   }
   // (no short runs, but one to be at hand, where the longest requests to be expected would not make any)
-  const int64_t shorts = longest < INT32_MAX && n_req * ((longest + 63) / 64) * v_heads <= kDpFew * at_once ? v_heads : kDpShorts * at_once;
+  const int64_t shorts = longest < INT32_MAX && n_req * ((longest + 63) / 64) * v_heads <= RunCuts::kFew * at_once ? v_heads : kDpShorts * at_once;
   return {0, at_once, (int32_t)std::max<int64_t>(1, at_once / v_heads), (int32_t)((shorts + v_heads - 1) / v_heads)};
 }
 
