@@ -417,7 +417,9 @@ purekv_status purekv_decode_paged(const void *q, int64_t q_token_stride, int64_t
  * The tensor-core prefill also checks the plan before using it (header, section offsets against the plan's size, every unit's and
  * entry's indices against the header's counts): on a mismatch nothing is read through the bad field, the status
  * word becomes PUREKV_ERR_BAD_PLAN and the output is undefined (untouched when the header itself fails).  After either code the plan's scheduling counters are
- * undefined: build the plan again before the next launch. */
+ * undefined: build the plan again before the next launch.
+ * The paged decode step waits for its copies and for the runs that it asks for; a CTA that gives up lets those in flight land and leaves.
+ * To it a limit below 1000 ns is no time at all: what is not there when it is asked about is late. */
 void purekv_set_wait_limit_ns(uint64_t ns);
 
 /* Synchronises `stream`, copies the device status word to *h_status_out and returns the code it holds

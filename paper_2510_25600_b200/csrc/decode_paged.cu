@@ -55,6 +55,8 @@ constexpr int kDpClusterMax = 16;
 constexpr int kDpGroups = 128;   // of requests: their running sums of tiles lie in shared memory
 constexpr int kDpSteals = 8;     // answers to requests for runs that a CTA keeps: more than runs its loads can be ahead of its products
 constexpr int kDpShorts = 3;     // short runs for every CTA at work
+constexpr uint64_t kDpNoWaitNs = 1000;           // limits below are no time at all: what is not there when it is asked about is late
+constexpr uint64_t kDpSettleNs = 1000000000ull;  // of the wait for what is in flight, before a CTA that gave up leaves
 
 // Tiles of one head: `left` of them, from tile `tile` of request r (n rows) on, tile `at` of the head's.
 struct DpRun {
@@ -599,6 +601,12 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   // The work at hand: `left` tiles from tile `tile` of (request r with n rows, virtual head vh) on.
   DpRun run = {};
   int32_t f_answers = 0;  // read so far
+  bool late = false;      // a wait of this warp's ran out: it asks for, loads and multiplies nothing any more
+  // Whether a barrier's phase has come, for the calling thread; false if the limit passes, or has passed for another thread of the CTA.
+  auto arrives = [&](uint32_t bar, uint32_t phase) {
+    if (a.wait_ns < kDpNoWaitNs) return tc::mbar_test(bar, phase);
+    return tc::mbar_try_wait(bar, phase) || tc::mbar_wait(bar, phase, &s_late, a.wait_ns);
+  };
   RunCuts cuts = {};
   auto take = [&](int32_t b) {
     const int32_t j = cuts.piece_of(b);
@@ -643,13 +651,9 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     tc::mbar_expect_tx(bar, 16);
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(slot), "r"(bar) : "memory");
   };
-  // The run of answer k, or -1.
+  // The run of answer k, -1 if there is none, -2 if the answer is late.
   auto answer = [&](int32_t k) {
-    volatile int late = 0;
-    if (!tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]), (uint32_t)(k / kDpSteals) & 1u, &late, a.wait_ns)) {
-      atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
-      return -1;
-    }
+    if (!arrives((uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]), (uint32_t)(k / kDpSteals) & 1u)) return -2;
     const volatile ulonglong2& h = s_stolen[k % kDpSteals];
     const uint64_t lo = h.x, hi = h.y;
     uint32_t yes, b;
@@ -663,10 +667,24 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   ChainRecord* const chains = reinterpret_cast<ChainRecord*>(a.chains);
   // The next run with tiles among those that no CTA has started, `k` answers having been read; without tiles if there are none.  One
   // thread asks for the block: the answers' slots are its own as long as no warp waits for one.
+  auto settle_answer = [&](int32_t k) {  // it comes into shared memory, which the CTA must not leave before
+    volatile int again = 0;
+    tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]), (uint32_t)(k / kDpSteals) & 1u, &again, kDpSettleNs);
+  };
   auto find = [&](int32_t& k) {
     if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again
     if (tid == 0) {
-      s_found[0] = next_run(cuts, [&] { ask(k); return answer(k++); }, [&](int32_t b) { chains[b].parts = 0; });
+      auto next = [&] {
+        ask(k);
+        const int32_t b = answer(k);
+        if (b == -2) {
+          atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
+          settle_answer(k);
+        }
+        ++k;
+        return b;
+      };
+      s_found[0] = next_run(cuts, next, [&](int32_t b) { chains[b].parts = 0; });
       s_found[1] = k;
     }
     __syncthreads();
@@ -724,14 +742,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (tid == 0) ask(f_answers);
   }
 
-  // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier).
+  // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier); the same for all its lanes.
   auto arrived = [&](int32_t stage, uint32_t phase) {
     if constexpr (LOAD == kDpEngine) {
-      const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]);
-      if (tc::mbar_try_wait(bar, phase) || tc::mbar_wait(bar, phase, &s_late, a.wait_ns)) return true;
-      atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
-      volatile int again = 0;  // the copies may still come: once more as long, before the stage is given up
-      return tc::mbar_wait(bar, phase, &again, a.wait_ns);
+      return __all_sync(0xffffffffu, arrives((uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), phase)) != 0;
     } else {
       asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
       return true;
@@ -754,10 +768,14 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   auto look = [&]() {
     Look k = {-1, 0, 0, 0};
     if constexpr (!CLUSTER) {
-      if (f.left == 0 && f_more) {
-        const int32_t b = answer(f_answers++);
-        f_more = false;
-        if (b >= 0) {
+      if (f.left == 0 && f_more && !late) {
+        const int32_t b = answer(f_answers);
+        late = __any_sync(0xffffffffu, b == -2);  // (for one lane, so for all: what follows is the warp's together)
+        if (!late) {
+          ++f_answers;
+          f_more = false;
+        }
+        if (!late && b >= 0) {
           if (tid == 0) chains[b].parts = 0;
           const DpRun x = take(b);
           if (x.left > 0) {
@@ -882,6 +900,20 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (lane == 0) s_mask[warp][stage] = mask;
     if constexpr (LOAD != kDpEngine) asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
   };
+  // A wait ran out: all of the CTA's threads leave, once what is under way into shared memory has landed, copies into the `stages` stages
+  // from `stage` on and an answer.
+  auto leave = [&](int32_t stages, int32_t stage, uint32_t phase) {
+    if (late && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
+    if constexpr (LOAD == kDpEngine) {
+      volatile int again = 0;
+      for (int32_t i = 0; i < stages; ++i, stage = stage + 1 == ST ? 0 : stage + 1, phase ^= stage == 0)
+        tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), phase, &again, kDpSettleNs);
+    } else {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    if (tid == 0 && f_more) settle_answer(f_answers);
+  };
+
   E e;
   auto heads_at = [&](int32_t v, int32_t& g, int32_t& h0, int32_t& nh) {
     g = a.blocks == 1 ? v : v / a.blocks;
@@ -906,7 +938,8 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   heads_at(run.vh, g, h0, nh);
   e.load(a, s_e, run.r, g, h0, nh);
   e.ready(s_e);
-  __syncthreads();
+  if constexpr (CLUSTER) __syncthreads();
+  else if (__syncthreads_or(late)) return leave(ST - 1, stage, phase);
   from_start = run.tile == 0;
   while (true) {
     bool end_of_request = true;
@@ -915,9 +948,11 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         fetch(stage == 0 ? ST - 1 : stage - 1, next);
         next = look();
       }
-      const bool ok = arrived(stage, phase);
+      late = late || !arrived(stage, phase);
       __syncwarp();
-      const Mask mask = ok ? s_mask[warp][stage] : (Mask)0;
+    }
+    if (run.left > 0 && !late) {
+      const Mask mask = s_mask[warp][stage];
       if constexpr (LOAD == kDpEngine) {
         constexpr Mask kAll = (Mask)(~(Mask)0 >> (8 * sizeof(Mask) - TK));
         if (mask != 0 && mask != kAll) {  // zeros for the values that are not the request's: whatever lies there has weight 0, but may be NaN
@@ -951,7 +986,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     }
 
     // ---- the warps' results side by side, each over the stage that its warp has just used up
-    e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
+    if (!late) e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
     const DpRun done = run;
     const int32_t h0_done = h0, nh_done = nh, g_done = g;
     bool more = false;
@@ -970,9 +1005,11 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         e.load(a, s_e, run.r, g, h0, nh);
       }
     }
-    __syncthreads();
     if constexpr (CLUSTER) {
+      __syncthreads();
       if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    } else {
+      if (__syncthreads_or(late)) return leave(ST, stage, phase);  // (the stage just used up, if there is one, is there)
     }
     const float vs = a.v_scale ? a.v_scale[g_done] : 1.f;
     const bool whole = CLUSTER ? C == 1 : from_start && end_of_request;

@@ -31,6 +31,16 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// The same without waiting at all.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // Whether two barriers' phases are complete, asked for together: one round trip instead of two.
 __device__ __forceinline__ void mbar_test2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, bool* done0,
                                            bool* done1) {
