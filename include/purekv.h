@@ -397,7 +397,7 @@ purekv_status purekv_compact_paged(const void *k, const void *v, int64_t layer_s
 
 /* purekv_decode_attention over the pages of one layer: one new query per request and head, every row of the request visible.
  * q [n_req, H, d] with strides, o [n_req, H, d] contiguous (may be q itself where that is contiguous), lse (nullable) [n_req, H].
- * A request with seq_lens[r] <= 0 gets o = 0 and lse = -inf.  head_dim 64 or 128; any number of query heads per KV head; dtype (q and o) BF16 with pools
+ * A request with seq_lens[r] <= 0, or none of whose keys is there or weighs anything, gets o = 0 and lse = -inf.  head_dim 64 or 128; any number of query heads per KV head; dtype (q and o) BF16 with pools
  * of BF16 or E4M3, or FP32 with FP32 pools.  max_len only sizes the launch: the longest request that is to be expected,
  * 0 if unknown; longer requests are served all the same.  ws: purekv_decode_paged_ws_bytes for the same sizes (nullable
  * when that is 0), not initialised; calls that may run at the same time need one each.  softmax_scale <= 0 means 1/sqrt(d).  Waits

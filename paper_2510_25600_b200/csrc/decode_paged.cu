@@ -534,6 +534,9 @@ struct ChainRecord {
 __device__ __forceinline__ float dp_weight(float m, float l, float ref) { return l == 0.f ? 0.f : dec_ex2(m - ref); }
 __device__ __forceinline__ float dp_seen(float m, float l) { return l == 0.f ? -INFINITY : m; }
 __device__ __forceinline__ float dp_finite(float m) { return m == -INFINITY ? 0.f : m; }
+// What a request's sums are multiplied by, and its log-sum-exp: 0 and -inf where no key weighs anything (no rows, or none that is there).
+__device__ __forceinline__ float dp_over(float scale, float l) { return l == 0.f ? 0.f : scale / l; }
+__device__ __forceinline__ float dp_lse(float ref, float l) { return (ref + log2f(l)) * 0.6931471805599453f; }
 
 template <typename T>
 __device__ __forceinline__ void dp_store4(T* dst, float4 v);
@@ -1033,9 +1036,9 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
       if (whole) {
         const int64_t hq = (int64_t)done.r * a.n_q_heads + h0_done + h;
-        const float inv = done.n > 0 ? vs / l : 0.f;
+        const float inv = dp_over(vs, l);
         dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + col, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-        if (col == 0 && a.lse) a.lse[hq] = done.n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (col == 0 && a.lse) a.lse[hq] = dp_lse(ref, l);
       } else if constexpr (CLUSTER) {
         const uint32_t to = (uint32_t)(col / cols);
         asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec_mapa(s_part + (rank * nh_done + h) * cols + col % cols, to)),
@@ -1125,9 +1128,9 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
       if (part == 0 && x < items) {
         const int64_t hq = (int64_t)run.r * a.n_q_heads + h0 + h;
-        const float inv = run.n > 0 ? vs / l : 0.f;
+        const float inv = dp_over(vs, l);
         dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + (rank * quads + c) * 4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-        if (rank == 0 && c == 0 && a.lse) a.lse[hq] = run.n > 0 ? (ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (rank == 0 && c == 0 && a.lse) a.lse[hq] = dp_lse(ref, l);
       }
     }
   }
@@ -1228,9 +1231,9 @@ __global__ void __launch_bounds__(256, OCC) decode_paged_join_kernel(const __gri
     }
     if (grp == 0 && h < nh) {
       const int64_t hq = (int64_t)chain.r * a.n_q_heads + g * a.group + b * R + h;
-      const float inv = (a.v_scale ? a.v_scale[g] : 1.f) / l;
+      const float inv = dp_over(a.v_scale ? a.v_scale[g] : 1.f, l);
       dp_store4(reinterpret_cast<Out*>(a.o) + hq * D + 4 * c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (c == 0 && a.lse) a.lse[hq] = (dp_finite(ref) + log2f(l)) * 0.6931471805599453f;
+      if (c == 0 && a.lse) a.lse[hq] = dp_lse(dp_finite(ref), l);
     }
   }
 }
