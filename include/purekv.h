@@ -424,8 +424,9 @@ void purekv_set_wait_limit_ns(uint64_t ns);
 
 /* Synchronises `stream`, copies the device status word to *h_status_out and returns the code it holds
  * (PUREKV_ERR_TIMEOUT, PUREKV_ERR_BAD_PLAN or PUREKV_ERR_BAD_PAGE) if it is non-zero, PUREKV_ERR_CUDA if the stream reported an error.
- * status == NULL polls the word inside the library that calls made with a NULL status use (one per
- * device, shared by all such calls) and clears it if it was raised.  A raised word makes every later
+ * status == NULL polls the words inside the library that calls made with a NULL status use (two per
+ * device: one shared by all such tensor-core prefill and score calls, one by all such paged calls), reports the first that is raised
+ * and clears it; if both are, the next poll reports the other.  A raised word makes every later
  * tensor-core prefill or score call that uses it return without computing -- the caller's own word stays raised until the caller
  * clears it, the library's until it is polled this way -- so poll after the calls whose results matter. */
 purekv_status purekv_poll_status(const int32_t *status, int32_t *h_status_out, void *stream);

@@ -42,9 +42,11 @@ purekv_status launch_compact(const void* k, const void* v, int64_t layer_stride,
                              const purekv_batch* batch, const int32_t* cu_kept, int32_t k_tot, int32_t n_kv_heads, int64_t row_bytes,
                              int64_t elem_bytes, void* k_out, void* v_out, int64_t out_layer_stride, cudaStream_t stream);
 
-// The status word a call uses when the caller passes none: one word per device inside the library, read and
-// cleared by purekv_poll_status(NULL, ...).  Its device address is looked up once per device.
-purekv_status default_status_word(int32_t** out);
+// The status word a call uses when the caller passes none: two words per device inside the library, read and
+// cleared by purekv_poll_status(NULL, ...).  The tensor-core kernels compute nothing while theirs is raised; the paged calls have one
+// of their own, so that a wrong page of one conversation stops nobody else's prefill.  Their device address is looked up once per device.
+enum OwnWord : int { kWordTensorCore = 0, kWordPaged = 1, kOwnWords = 2 };
+purekv_status default_status_word(OwnWord which, int32_t** out);
 
 // Raises a kernel's dynamic shared-memory limit to what the device's opt-in maximum leaves, once per (kernel, device): `done`
 // is a bit mask over device ordinals that the call site keeps in a function-local static.  Launches then pass

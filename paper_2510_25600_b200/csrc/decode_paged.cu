@@ -1470,7 +1470,7 @@ purekv_status purekv_decode_paged(const void* q, int64_t q_token_stride, int64_t
     a.part = (float*)(a.chains + (int64_t)a.v_heads * (a.n_long + a.n_short) * (sizeof(ChainRecord) / 4));
   }
   if (!status) {
-    const purekv_status s2 = default_status_word(&a.status);
+    const purekv_status s2 = default_status_word(kWordPaged, &a.status);
     if (s2 != PUREKV_OK) return s2;
   }
   cudaStream_t sm = (cudaStream_t)stream;

@@ -483,7 +483,7 @@ purekv_status purekv_append_paged(const void* q, int64_t q_token_stride, int64_t
     a.store = pages->n_req > 0;
     a.status = status;
     if (!status) {
-      const purekv_status st = default_status_word(&a.status);
+      const purekv_status st = default_status_word(kWordPaged, &a.status);
       if (st != PUREKV_OK) return st;
     }
   }
@@ -549,7 +549,7 @@ purekv_status purekv_compact_paged(const void* k, const void* v, int64_t layer_s
   a.chunks = (int32_t)(pages->head_dim * esz / 16);
   a.status = status;
   if (!status) {
-    const purekv_status s2 = default_status_word(&a.status);
+    const purekv_status s2 = default_status_word(kWordPaged, &a.status);
     if (s2 != PUREKV_OK) return s2;
   }
   cudaStream_t sm = (cudaStream_t)stream;

@@ -79,11 +79,11 @@ static purekv_status check_params(const purekv_batch* b, const purekv_st_params*
 
 struct Span { int32_t a, b; };  // inclusive request-relative positions
 
-// The status word of calls made without one.  In host code this name is only a stand-in for the symbol: the device
+// The status words of calls made without one.  In host code this name is only a stand-in for the symbol: the device
 // address comes from cudaGetSymbolAddress, once per device.
-static __device__ int32_t g_default_status;
+static __device__ int32_t g_default_status[kOwnWords];
 
-purekv_status default_status_word(int32_t** out) {
+purekv_status default_status_word(OwnWord which, int32_t** out) {
   constexpr int kMaxDevices = 64;
   static std::mutex mu;
   static int32_t* ptrs[kMaxDevices] = {};
@@ -97,7 +97,7 @@ purekv_status default_status_word(int32_t** out) {
     PK_REQUIRE(p != nullptr, PUREKV_ERR_CUDA, "cudaGetSymbolAddress returned a null status address");
     ptrs[dev] = p;
   }
-  *out = ptrs[dev];
+  *out = ptrs[dev] + which;
   return PUREKV_OK;
 }
 
@@ -777,13 +777,14 @@ purekv_status purekv_poll_status(const int32_t* status, int32_t* h_out, void* st
   if (status) {
     PK_CUDA(cudaMemcpy(&v, status, sizeof(v), cudaMemcpyDeviceToHost));
   } else {
-    // the library's own word, used by calls made with status == NULL: report it and clear it, so that one expired
+    // the library's own words, used by calls made with status == NULL: report one that is raised and clear it, so that one expired
     // wait does not block every later call of that kind
-    int32_t* own = nullptr;
-    purekv_status st = default_status_word(&own);
+    int32_t *own = nullptr, held[kOwnWords] = {};
+    purekv_status st = default_status_word(kWordTensorCore, &own);
     if (st != PUREKV_OK) return st;
-    PK_CUDA(cudaMemcpy(&v, own, sizeof(v), cudaMemcpyDeviceToHost));
-    if (v != 0) PK_CUDA(cudaMemset(own, 0, sizeof(v)));
+    PK_CUDA(cudaMemcpy(held, own, sizeof(held), cudaMemcpyDeviceToHost));
+    for (int which = 0; which < kOwnWords && v == 0; ++which)
+      if ((v = held[which]) != 0) PK_CUDA(cudaMemset(own + which, 0, sizeof(v)));
   }
   if (h_out) *h_out = v;
   PK_REQUIRE(v != (int32_t)PUREKV_ERR_BAD_PLAN, PUREKV_ERR_BAD_PLAN,

@@ -1047,7 +1047,7 @@ purekv_status launch_prefill_tc(const PrefillArgs& a) {
   if ((st = make_map_layers(&mo, a.o, T, a.n_q_heads, kBQ, L, L > 1 ? a.o_stride : T * a.n_q_heads * kD)) != PUREKV_OK) return st;
   int32_t* status = a.status;
   if (!status) {
-    const purekv_status st_w = default_status_word(&status);
+    const purekv_status st_w = default_status_word(kWordTensorCore, &status);
     if (st_w != PUREKV_OK) return st_w;
   }
   return launch(a, mq, mk, mv, mk64, mv64, mo, status);

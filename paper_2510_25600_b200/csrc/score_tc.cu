@@ -624,7 +624,7 @@ extern "C" purekv_status purekv_lowlayer_score_lse(const void* q, const void* k,
   if ((st = make_map(&mk, k, T, n_kv_heads, kKeys)) != PUREKV_OK) return st;
   if ((st = make_map(&mq8, q, T, n_q_heads, box_rows)) != PUREKV_OK) return st;
   if (!status) {
-    const purekv_status st_w = default_status_word(&status);
+    const purekv_status st_w = default_status_word(kWordTensorCore, &status);
     if (st_w != PUREKV_OK) return st_w;
   }
   const size_t smem = 1024 + (size_t)(1 + kStages) * kTile;
