@@ -4,7 +4,7 @@ Every function here has the name of the C entry point it calls and passes torch
 tensors' device pointers straight through, the hot ones by way of the native module
 `_marshal` or, the paged calls, `_paged`, the others with ctypes; no step of the method runs in Python or in
 torch.  torch supplies device memory and the current CUDA stream.  Importing
-this module raises if the compiled library is missing: there is no fallback path.
+this module raises if the compiled library or `_marshal` is missing, a paged call if `_paged` is: there is no fallback path.
 """
 from __future__ import annotations
 
@@ -36,9 +36,20 @@ def _load_paged():
     try:
         module = importlib.util.module_from_spec(spec)
     except ImportError as e:
-        raise ImportError(f"{_HERE} holds no _paged module for this Python and torch: build it with `python -m paper_2510_25600_b200.build`") from e
+        return _NoPaged(e)
     spec.loader.exec_module(module)
     return module
+
+
+class _NoPaged:
+    """Stands for `_paged` where there is none for this torch: the paged calls raise, and no other call needs it."""
+
+    def __init__(self, cause: ImportError):
+        self._cause = cause
+
+    def __getattr__(self, call: str):
+        raise ImportError(f"{call}: {_HERE} holds no _paged module for this Python and torch: build it with `python -m paper_2510_25600_b200.build`") \
+            from self._cause
 
 
 _paged = _load_paged()

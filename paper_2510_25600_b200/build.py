@@ -82,7 +82,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", INCLUDE,
                                src, "-o", MARSHAL, "-L", _HERE, "-l:libpurekv.so", "-Wl,-rpath,$ORIGIN"])
     src = os.path.join(CSRC, "paged_py.cpp")
-    if force or _stale(PAGED, [src, LIB, os.path.join(INCLUDE, "purekv.h")]):
+    if not os.path.exists(os.path.join(_TORCH, "lib", "libc10_cuda.so")):
+        sys.stderr.write("a torch without CUDA: _paged is not built, and the paged calls will raise\n")
+    elif force or _stale(PAGED, [src, LIB, os.path.join(INCLUDE, "purekv.h")]):
         cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
         includes = [sysconfig.get_paths()["include"], INCLUDE, os.path.join(_TORCH, "include"),
                     os.path.join(_TORCH, "include", "torch", "csrc", "api", "include"), cuda]
