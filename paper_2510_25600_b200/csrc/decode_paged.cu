@@ -1376,7 +1376,9 @@ template <class E, class X, int ST8, int ST4, int OCC4>
 static purekv_status launch_rows(const DecodePagedArgs& a, int32_t n_kv_heads, const DpForm& f, cudaStream_t stream) {
   const bool whole = a.view.page_size.d % E::TK == 0;
   if (f.cluster && f.per_sm == 3) return launch_even<E, 4, 1, kDpRows, (E::R > 8 ? 2 : 3)>(a, f.cluster, stream);
-  if (f.cluster && f.per_sm == 4) return launch_even<E, 8, 1, kDpRows, (E::R > 8 ? 1 : 2)>(a, f.cluster, stream);
+  if constexpr (E::RowBytes < 4 * E::D) {  // (dp_form has no such CTAs for fp32)
+    if (f.cluster && f.per_sm == 4) return launch_even<E, 8, 1, kDpRows, (E::R > 8 ? 1 : 2)>(a, f.cluster, stream);
+  }
   if (f.cluster && f.per_sm == 2) return launch_even<E, 4, (OCC4 == 3 ? 2 : 3), kDpRows, OCC4>(a, f.cluster, stream);
   if (f.cluster) return whole ? launch_even<E, 8, ST8, kDpWhole, 1>(a, f.cluster, stream) : launch_even<E, 8, ST8, kDpRows, 1>(a, f.cluster, stream);
   DpMaps maps = {};
