@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
   const int64_t tok_stride = is_q ? a.q_tok : is_v ? a.v_tok : a.k_tok;
   const uint8_t* src = (is_q ? a.q + h * a.q_head : is_v ? a.v + h * a.v_head : a.k + h * a.k_head) + t0 * tok_stride;
   const int32_t rc = a.half / E;  // chunks of the first halves (half-split pairs)
-  const bool split = turns && !a.interleaved && j < rc;
+  const bool rotates = turns && j < rc;  // (of the row's chunks 2 rc hold what turns; interleaved, its chunks 2 j and 2 j + 1 hold whole pairs)
+  const bool split = rotates && !a.interleaved;
   const int32_t ca = split ? j : 2 * j, cb = split ? j + rc : 2 * j + 1;  // (2 rc + 2 (j - rc) = 2 j past the halves)
   uint4 ux[TOK], uy[TOK];
 #pragma unroll
@@ -184,13 +185,13 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
         x[e] = xe * w.x - ye * w.y;
         y[e] = ye * w.x + xe * w.y;
       }
-    } else if (turns && a.interleaved) {
+      ux[u] = Chunk<T>::put(x);  // (what does not turn stays as it is, a NaN's bits too)
+      uy[u] = Chunk<T>::put(y);
+    } else if (rotates) {
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
         auto rotate = [&](float (&z)[E], int32_t c) {
-          const int32_t pair = (c * E + e) / 2;
-          if (pair >= a.half) return;
-          const float2 w = turn[pair];
+          const float2 w = turn[(c * E + e) / 2];
           const float ze = z[e], zo = z[e + 1];
           z[e] = ze * w.x - zo * w.y;
           z[e + 1] = zo * w.x + ze * w.y;
@@ -198,13 +199,13 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
         rotate(x, ca);
         rotate(y, cb);
       }
+      ux[u] = Chunk<T>::put(x);
+      uy[u] = Chunk<T>::put(y);
     }
-    const bool changed = split || (turns && a.interleaved);  // (what is copied stays as it is, a NaN's bits too)
-    const uint4 px = changed ? Chunk<T>::put(x) : ux[u], py = changed ? Chunk<T>::put(y) : uy[u];
     if (out) {
       uint4* o4 = reinterpret_cast<uint4*>(out + (t0 + u) * out_tok + h * out_row);
-      o4[ca] = px;
-      o4[cb] = py;
+      o4[ca] = ux[u];
+      o4[cb] = uy[u];
     }
     if (store && s_dst[u] >= 0) {
       uint8_t* dst = pool + s_dst[u];
@@ -212,8 +213,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
         reinterpret_cast<uint2*>(dst)[ca] = to_e4m3(x, inverse);
         reinterpret_cast<uint2*>(dst)[cb] = to_e4m3(y, inverse);
       } else {
-        reinterpret_cast<uint4*>(dst)[ca] = px;
-        reinterpret_cast<uint4*>(dst)[cb] = py;
+        reinterpret_cast<uint4*>(dst)[ca] = ux[u];
+        reinterpret_cast<uint4*>(dst)[cb] = uy[u];
       }
     }
   }
