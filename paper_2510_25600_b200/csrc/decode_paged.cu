@@ -607,8 +607,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   bool late = false;      // a wait of this warp's ran out: it asks for, loads and multiplies nothing any more
   // Whether a barrier's phase has come, for the calling thread; false if the limit passes, or has passed for another thread of the CTA.
   auto arrives = [&](uint32_t bar, uint32_t phase) {
-    if (a.wait_ns < kDpNoWaitNs) return tc::mbar_test(bar, phase);
-    return tc::mbar_try_wait(bar, phase) || tc::mbar_wait(bar, phase, &s_late, a.wait_ns);
+    if (tc::mbar_test(bar, phase)) return true;
+    if (a.wait_ns >= kDpNoWaitNs) return tc::mbar_wait(bar, phase, &s_late, a.wait_ns);
+    *(volatile int*)&s_late = 1;
+    return false;
   };
   RunCuts cuts = {};
   auto take = [&](int32_t b) {
@@ -678,7 +680,6 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again
     if (tid == 0) {
       auto next = [&] {
-        ask(k);
         const int32_t b = answer(k);
         if (b == -2) {
           atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
@@ -687,7 +688,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         ++k;
         return b;
       };
-      s_found[0] = next_run(cuts, next, [&](int32_t b) { chains[b].parts = 0; });
+      s_found[0] = next_run(cuts, [&] { ask(k); }, next, [&](int32_t b) { chains[b].parts = 0; });
       s_found[1] = k;
     }
     __syncthreads();
@@ -745,10 +746,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (tid == 0) ask(f_answers);
   }
 
-  // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier); the same for all its lanes.
+  // Whether this warp's copies into `stage` have arrived (phase: of the stage's barrier), for the calling lane.
   auto arrived = [&](int32_t stage, uint32_t phase) {
     if constexpr (LOAD == kDpEngine) {
-      return __all_sync(0xffffffffu, arrives((uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), phase)) != 0;
+      return arrives((uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), phase);
     } else {
       asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
       return true;
@@ -903,13 +904,13 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     if (lane == 0) s_mask[warp][stage] = mask;
     if constexpr (LOAD != kDpEngine) asm volatile("cp.async.commit_group;" ::: "memory");  // (empty past the end: the group count stays in step)
   };
-  // A wait ran out: all of the CTA's threads leave, once what is under way into shared memory has landed, copies into the `stages` stages
-  // from `stage` on and an answer.
-  auto leave = [&](int32_t stages, int32_t stage, uint32_t phase) {
+  // A wait ran out: all of the CTA's threads leave, once what is under way into shared memory has landed, copies into any stage (into the
+  // one just used up, `stage`, they have unless they are the late ones) and an answer.
+  auto leave = [&](int32_t stage, uint32_t phase) {
     if (late && lane == 0) atomicExch(a.status, (int32_t)PUREKV_ERR_TIMEOUT);
     if constexpr (LOAD == kDpEngine) {
       volatile int again = 0;
-      for (int32_t i = 0; i < stages; ++i, stage = stage + 1 == ST ? 0 : stage + 1, phase ^= stage == 0)
+      for (int32_t i = 0; i < ST; ++i, stage = stage + 1 == ST ? 0 : stage + 1, phase ^= stage == 0)
         tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_full[warp][stage]), phase, &again, kDpSettleNs);
     } else {
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -941,8 +942,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
   heads_at(run.vh, g, h0, nh);
   e.load(a, s_e, run.r, g, h0, nh);
   e.ready(s_e);
-  if constexpr (CLUSTER) __syncthreads();
-  else if (__syncthreads_or(late)) return leave(ST - 1, stage, phase);
+  __syncthreads();
   from_start = run.tile == 0;
   while (true) {
     bool end_of_request = true;
@@ -951,10 +951,8 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         fetch(stage == 0 ? ST - 1 : stage - 1, next);
         next = look();
       }
-      late = late || !arrived(stage, phase);
+      late = late || !arrived(stage, phase);  // (if so the tile is whatever lies there, and the warp's last one)
       __syncwarp();
-    }
-    if (run.left > 0 && !late) {
       const Mask mask = s_mask[warp][stage];
       if constexpr (LOAD == kDpEngine) {
         constexpr Mask kAll = (Mask)(~(Mask)0 >> (8 * sizeof(Mask) - TK));
@@ -971,6 +969,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
       }
       if (mask) e.trip(ring + (uint32_t)stage * kStage, mask, s_e, warp);
       __syncwarp();  // every lane has read the stage before the next fetch overwrites it
+      if constexpr (!CLUSTER) late = __any_sync(0xffffffffu, late);
       --run.left;
       ++run.at;
       end_of_request = ++run.tile == tiles_of(run.n);
@@ -981,7 +980,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
           next = look();
         }
       }
-      if (!end_of_request && run.left > 0) {
+      if (!end_of_request && run.left > 0 && !late) {
         stage = stage + 1 == ST ? 0 : stage + 1;
         phase ^= stage == 0;
         continue;
@@ -989,7 +988,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     }
 
     // ---- the warps' results side by side, each over the stage that its warp has just used up
-    if (!late) e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
+    e.finish(reinterpret_cast<float*>(dp_smem + warp * kWarpBytes + stage * kStage), LD, s_ml[warp]);
     const DpRun done = run;
     const int32_t h0_done = h0, nh_done = nh, g_done = g;
     bool more = false;
@@ -1008,11 +1007,10 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         e.load(a, s_e, run.r, g, h0, nh);
       }
     }
+    __syncthreads();
+    const bool quit = !CLUSTER && *(volatile int*)&s_late;  // a warp's wait ran out: the results are nobody's (no warp waits again before the next barrier)
     if constexpr (CLUSTER) {
-      __syncthreads();
       if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    } else {
-      if (__syncthreads_or(late)) return leave(ST, stage, phase);  // (the stage just used up, if there is one, is there)
     }
     const float vs = a.v_scale ? a.v_scale[g_done] : 1.f;
     const bool whole = CLUSTER ? C == 1 : from_start && end_of_request;
@@ -1060,6 +1058,7 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
         const int64_t last = done.at - 1 + (tiles_of(done.n) - done.tile);
         chains[done.id] = {done.r, done.vh, cuts.piece_with(last) - cuts.piece_of(done.id) + 1, 0};
       }
+      if (quit) return leave(stage, phase);
       if (!more) break;
       e.ready(s_e);
       if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again

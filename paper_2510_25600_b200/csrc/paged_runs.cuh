@@ -16,8 +16,13 @@ struct RunCuts {
   int32_t v_heads, n_long, n_short;
 
   static PK_HD RunCuts of(int64_t all, int32_t v_heads, int32_t at_once, int32_t n_long, int32_t n_short) {
-    const int64_t share = all * v_heads * 3 / 4 / at_once;
-    const int64_t lt = all * v_heads <= (int64_t)kFew * at_once ? (all + n_long - 1) / n_long : share < 1 ? 1 : share < all ? share : all;
+    int64_t lt;
+    if (all * v_heads <= (int64_t)kFew * at_once) {
+      lt = (all + n_long - 1) / n_long;
+    } else {
+      lt = all * v_heads * 3 / 4 / at_once;
+      lt = lt < 1 ? 1 : lt < all ? lt : all;
+    }
     const int64_t rest = all - n_long * lt, st = rest > 0 ? (rest + n_short - 1) / n_short : 0;
     return {all, lt, st > kShortest ? st : kShortest, v_heads, n_long, n_short};
   }
@@ -26,6 +31,8 @@ struct RunCuts {
     const int64_t t = piece <= n_long ? piece * long_tiles : n_long * long_tiles + (piece - n_long) * short_tiles;
     return t < all ? t : all;
   }
+  // the runs before this one have tiles, it and those behind it none
+  PK_HD int32_t first_empty() const { return all > 0 ? (piece_with(all - 1) + 1) * v_heads : 0; }
   PK_HD int64_t tiles(int32_t run) const { return starts_at(piece_of(run) + 1) - starts_at(piece_of(run)); }
   // the piece of a head that has tile `tile`
   PK_HD int32_t piece_with(int64_t tile) const {
@@ -33,14 +40,15 @@ struct RunCuts {
   }
 };
 
-// Takes runs that no CTA has started, in whatever order they come, until one has tiles; -1 once there are none.  `take` returns a run
-// or -1, `taken` is told of each.
-template <typename Take, typename Taken>
-PK_HD int32_t next_run(const RunCuts& cuts, Take take, Taken taken) {
-  int32_t b;
-  while ((b = take()) >= 0) {
+// Takes runs that no CTA has started, in whatever order they come, until one has tiles; -1 once there are none.  `ask` asks for one,
+// `answer` returns it, or -1, and `taken` is told of each.
+template <typename Ask, typename Answer, typename Taken>
+PK_HD int32_t next_run(const RunCuts& cuts, Ask ask, Answer answer, Taken taken) {
+  ask();
+  const int32_t empty = cuts.first_empty();  // (while the answer is under way)
+  for (int32_t b; (b = answer()) >= 0; ask()) {
     taken(b);
-    if (cuts.tiles(b) > 0) return b;
+    if (b < empty) return b;
   }
   return -1;
 }

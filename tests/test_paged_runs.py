@@ -31,7 +31,10 @@ int main(int, char** v) {
   }
   if (at != all) return printf("%lld tiles of %lld", (long long)at, (long long)all), 0;
   std::vector<int32_t> pending, taken(runs), told(runs);
-  for (int32_t b = 0; b < runs; ++b) pending.push_back(b);
+  for (int32_t b = 0; b < runs; ++b) {
+    if ((b < cuts.first_empty()) != (cuts.tiles(b) > 0)) return printf("tiles of run %d", b), 0;
+    pending.push_back(b);
+  }
   uint32_t x = 12345;
   auto any = [&] {
     if (pending.empty()) return -1;
@@ -44,7 +47,7 @@ int main(int, char** v) {
   };
   auto find = [&] {
     if (discard) { while (any() >= 0) {} return -1; }
-    return next_run(cuts, any, [](int32_t) {});
+    return next_run(cuts, [] {}, any, [](int32_t) {});
   };
   struct Cta { int32_t run; bool more, empty; };
   std::vector<Cta> ctas;
