@@ -7,14 +7,21 @@
 // Two kernels share everything but the way work reaches a CTA:
 //  * even (CLUSTER): grid (C, heads, requests); a cluster of C CTAs owns one (request, KV head) and its parts meet in distributed
 //    shared memory.  One launch, no workspace.
-//  * balanced: one wave of persistent CTAs; the (KV head, request, tile of keys) triples in that order are cut into equal runs, whatever
-//    the lengths are -- they are read on the device -- and a run goes on loading across the ends of requests.  (Head by head, so that
-//    CTAs at work on the heads of a request are at the same rows at the same time: those lie side by side in memory.)  A request that a cut
-//    goes through leaves partial results in the workspace, which a second, small kernel joins.
+//  * balanced: the (KV head, request, tile of keys) triples in that order are cut into runs, whatever the lengths are -- they are read on
+//    the device -- and a block is launched for each: first the long runs, as many as CTAs are at work at once, then the short ones
+//    (paged_runs.cuh).  A CTA that comes to the end of its run takes over a block that has not started (cluster launch control), since
+//    SMs do not stream equally fast, and goes on loading across the ends of requests and runs.  In which order blocks start and are handed
+//    out does not matter.  (Head by head, so that CTAs at work on the heads of a request are at the same rows at the same time: those lie
+//    side by side in memory.)  A request that a cut goes through leaves partial results in the workspace, which a second, small kernel joins.
 //
-// Inside a CTA every warp takes TK keys of a tile at a time through a ring of its own in shared memory (cp.async, ST stages), looks the
-// pages of its next keys up one step ahead, and keeps (reference maximum, sum, unnormalised output) in registers; the warps' results are
-// joined at the end of a request.  Rows that do not exist are not read and weigh nothing.
+// Inside a CTA every warp takes TK keys of a tile at a time through a ring of its own in shared memory (ST stages), filled by the copy
+// engine (balanced form, pages that hold whole trips or of which a trip holds several) or by cp.async, looks the pages of its next keys up
+// one step ahead, and keeps (reference maximum, sum, unnormalised output) in registers; the warps' results are joined at the end of a
+// request.  Rows that do not exist are not read and weigh nothing.
+//
+// Waits on copies and answers are bounded.  A lane whose wait runs out goes on to the end of the tile, with whatever lies there; there its
+// warp agrees to stop, and at the barrier at the request's end the CTA does: no vote or matrix product is reached by some lanes only.
+// The CTA leaves once what is under way into its shared memory has landed.
 #include <algorithm>
 #include <cmath>
 
@@ -165,7 +172,10 @@ struct MaskOf { using type = uint32_t; };
 template <>
 struct MaskOf<64> { using type = uint64_t; };
 
-// bf16 pools.  Padding of 16 bytes, so that ldmatrix reads eight rows without bank conflicts.
+// bf16 pools.  Padding of 16 bytes, so that ldmatrix reads eight rows without bank conflicts.  The weights are rounded to bf16 for the
+// product with the values, as tiles have one type, and their sum is not: 2^-8 of each at most, independent of one another, 0.8e-3 of the
+// result's norm beside the 1.7e-3 of its own rounding (1.9e-3 together).  What rounding leaves of the weights, as a second product, would
+// remove that for twice the products with the values.
 template <int D_, int NT, int MT, bool SW_>
 struct Bf16Rows {
   static constexpr bool SW = SW_;
@@ -1322,7 +1332,9 @@ struct DpForm {
 // a head's rows (200 bf16 rows: 4.7 with one CTA, 5.0 with 4; 500: 7.3 and 5.1), and no pairs for less than 200 KB (64 heads of 300
 // rows: 6.2 alone, 6.9 in pairs; of 500 7.8 and 6.9).  Balanced from 380 MB on, which is 60 us: the even form may still be level there if all
 // requests are as long as the longest, but nothing says so (128 of 2900-5100 rows: 167 against 173; one of 60 000 among 63 of 100-2000: 57
-// against 450), and where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 33 against 34).
+// against 450), and where the even form's longest share takes longer (one request of 64 000 rows, 4 heads: 39 against 36, in e4m3 26 and 25).  Lengths are
+// unknown here but for the longest: a batch with one long request among short ones is taken for as much work as if all were as long (63 of 200
+// rows and one of 6000, one head: 28, 17 in the balanced form, which a hint of 0 gives).
 static DpForm dp_form(int64_t n_req, int64_t v_heads, int64_t longest, int32_t head_dim, purekv_dtype held, int32_t at_once) {
   const int64_t row_bytes = 2 * head_dim * bytes_of(held);
   const int64_t base = n_req * v_heads, bytes = longest * row_bytes;  // of one head's rows
