@@ -680,12 +680,13 @@ __global__ void __launch_bounds__(W * 32, OCC) decode_paged_kernel(const __grid_
     return yes ? (int32_t)b : -1;
   };
   ChainRecord* const chains = reinterpret_cast<ChainRecord*>(a.chains);
-  // The next run with tiles among those that no CTA has started, `k` answers having been read; without tiles if there are none.  One
-  // thread asks for the block: the answers' slots are its own as long as no warp waits for one.
-  auto settle_answer = [&](int32_t k) {  // it comes into shared memory, which the CTA must not leave before
+  // Answer k has come into shared memory, which the CTA must not leave before.
+  auto settle_answer = [&](int32_t k) {
     volatile int again = 0;
     tc::mbar_wait((uint32_t)__cvta_generic_to_shared(&s_answered[k % kDpSteals]), (uint32_t)(k / kDpSteals) & 1u, &again, kDpSettleNs);
   };
+  // The next run with tiles among those that no CTA has started, `k` answers having been read; without tiles if there are none.  One
+  // thread asks for the block: the answers' slots are its own as long as no warp waits for one.
   auto find = [&](int32_t& k) {
     if constexpr (LOAD == kDpEngine) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the rows laid over the stages, before they are copied into again
     if (tid == 0) {
